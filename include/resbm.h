@@ -58,6 +58,7 @@ extern "C" {
 #define RESBM_E_ACT        -5  /* unknown act, or SiLU backward without a_save  */
 #define RESBM_E_HIP        -6  /* a kernel launch failed                        */
 #define RESBM_E_ALIAS      -7  /* an output aliases an input it may not alias   */
+#define RESBM_E_KIND       -8  /* unknown element type or state form, no plan   */
 
 #define RESBM_ACT_IDENTITY  0
 #define RESBM_ACT_SILU      1  /* phi(a) = a * sigmoid(a)                        */
@@ -376,6 +377,151 @@ int32_t resbm_decode_qkv_fwd(int64_t T, int32_t n, int32_t r, int32_t N,
                              const void* b, const float* W_d, const float* gamma,
                              const void* W_qkv, float eps, void* out, int64_t ld_out,
                              void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The residual stream and its RMS norm.  With the decoder's identity path
+ * added by the caller (reading B), a layer's output x, the stream res and the
+ * payload's skip b I_{r x n} (Eq. 5) are summed and the next layer begins
+ * with the norm of the sum:
+ *     h = x + res + b I_{r x n}
+ *     y[t][c] = h[t][c] rstd[t] gamma[c],  rstd[t] = 1 / sqrt(mean_c h[t][c]^2 + eps)
+ * The sum is formed in float32 in that order and rounded once to act; the norm
+ * is that of the rounded h, whether h is written or not, in float32 (a row
+ * whose mean square exceeds float32's range gets rstd = 0); y is rounded once.
+ *  x      T x n act, row stride ld_x.
+ *  res    T x n act, row stride ld_res, or NULL.
+ *  b      T x r act, packed [T][r]; r == 0: none (b may be NULL).
+ *  gamma  n float32.
+ *  h      out, T x n act, row stride ld_h, or NULL; may take the place of x or
+ *         res (same pointer and row stride).
+ *  y      out, T x n act, row stride ld_y.
+ *  rstd   out, T float32 (saved for resbm_skip_norm_bwd), or NULL.
+ * Shape rules of these ops: 0 <= T < 2^31; n % 8 == 0, 8 <= n <= 65536;
+ * r % 4 == 0, 0 <= r <= n; eps >= 0, finite; every leading dimension >= n
+ * and a multiple of 8.  gamma, dgamma, y and the activations 16-byte aligned.
+ */
+int32_t resbm_skip_norm_fwd(int64_t T, int32_t n, int32_t r,
+                            const void* x, int64_t ld_x, const void* res, int64_t ld_res,
+                            const void* b, const float* gamma, float eps,
+                            void* h, int64_t ld_h, void* y, int64_t ld_y,
+                            float* rstd, void* stream);
+
+/*
+ * The same with y in 8 bits (e4m3, largest value 448) and a float32 scale for
+ * every `group` columns of a row: group is 32, 64, 128 or 256 and divides n,
+ * or is n (one scale a row).  With a = max |y| over the group, y in float32,
+ *     scale = max(a (1 / 448), 2^-126),   code = e4m3(y (1 / scale)),  to nearest even
+ * (both reciprocals rounded to float32), so code * scale stands for y.  A group that holds an infinity or a NaN has
+ * that for its scale, and all of its values read back as NaN.
+ *  y      out, T x n bytes, row stride ld_y (ld_y >= n, ld_y % 8 == 0).
+ *  scale  out, T x (n / group) float32, packed.
+ */
+int32_t resbm_skip_norm_q8_fwd(int64_t T, int32_t n, int32_t r, int32_t group,
+                               const void* x, int64_t ld_x, const void* res, int64_t ld_res,
+                               const void* b, const float* gamma, float eps,
+                               void* h, int64_t ld_h, void* y, int64_t ld_y, float* scale,
+                               float* rstd, void* stream);
+
+/*
+ * Adjoint of resbm_skip_norm_fwd, with xh = h rstd and w = g_y gamma:
+ *     g_x = rstd (w - xh mean_c(w xh)) + g_h
+ *     dgamma = sum_t g_y xh   (+ the previous dgamma when accumulate != 0)
+ * g_x is the gradient of x and of res alike, and its columns [0, r) are the
+ * payload's: resbm_decode_bwd takes it as g_id.
+ *  h      T x n act: the forward's h (x itself where nothing was added).
+ *  rstd   T float32 from the forward.
+ *  g_y    T x n act, row stride ld_gy.
+ *  g_h    T x n act, row stride ld_gh: the gradient that reaches h past the
+ *         norm, or NULL.
+ *  g_x    out, T x n act, row stride ld_gx; may take the place of g_y or g_h.
+ *  dgamma n float32, overwritten or accumulated into; fixed order of the token
+ *         sum.  (T == 0 leaves it as it is, as in every op.)
+ *  ws     at least resbm_norm_workspace_bytes(T, n) bytes.
+ */
+size_t resbm_norm_workspace_bytes(int64_t T, int32_t n);
+int32_t resbm_skip_norm_bwd(int64_t T, int32_t n, const void* h, int64_t ld_h,
+                            const float* gamma, const float* rstd,
+                            const void* g_y, int64_t ld_gy, const void* g_h, int64_t ld_gh,
+                            void* g_x, int64_t ld_gx, float* dgamma, int32_t accumulate,
+                            void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * AdamW over many tensors at once: the optimizer step of the parameters that
+ * resbm_muon_update does not take (gains, projections, embeddings).  A plan
+ * lists the tensors; one launch then updates all of them:
+ *     g' = s g                      (s = *grad_scale, when grad_scale != NULL)
+ *     m <- b1 m + (1 - b1) g'       v <- b2 v + (1 - b2) g' g'
+ *     p <- (1 - lr wd) p - lr / (1 - b1^step) m / (sqrt(v) / sqrt(1 - b2^step) + eps)
+ * in float32, every operation rounded once.  Per tensor of numel elements:
+ *  p       float32 master, updated in place.
+ *  g       gradient, g_type RESBM_TYPE_F32 or RESBM_TYPE_BF16.
+ *  copy    bf16 working copy of p (what the resbm2_* and fused ops take),
+ *          written after the step; or NULL.
+ *  weight_decay  wd, >= 0.
+ *  state   RESBM_STATE_F32: m and v are float32, m_scale and v_scale unused.
+ *          RESBM_STATE_E4M3: one byte an element and one float32 scale for
+ *          each 256 elements (ceil(numel / 256) of them, the last for fewer):
+ *          m as code * m_scale, and u = sqrt(v) as code * v_scale, with
+ *          scale = max(max|.| (1 / 448), 2^-126) and code = e4m3(. (1 / scale)), to
+ *          nearest even, where a non-zero u takes the smallest non-zero code
+ *          rather than zero.  The step uses the new m and v before that
+ *          rounding.  All zeros are a valid start.  A non-finite element makes
+ *          its 256 elements' states non-finite.
+ * Pointers aligned to their elements; tensors whose p, g, m, v and copy are
+ * 16-byte aligned take wide accesses.  numel == 0 is an entry without work.
+ *
+ * resbm_adamw_plan checks a list (types, NULLs, alignment, and that nothing
+ * that a step writes overlaps anything else in the list) and writes the plan
+ * to host memory, 8-byte aligned, resbm_adamw_plan_bytes bytes (0 for an
+ * invalid list).  The caller copies it to device memory, 256-byte aligned, and
+ * passes both; it holds addresses, so it is valid while the tensors live.
+ * Entries that all have only g and numel make a plan for resbm_grad_norm
+ * alone.  RESBM_E_WORKSPACE: plan_bytes too small, or no host memory for the
+ * check.
+ *
+ *  lr_step  NULL, or a device array {lr, step} of two float64 that replaces
+ *           the arguments of those names, read when the kernel runs: for a
+ *           captured step that is replayed with other values.
+ *  grad_scale  NULL, or one device float32, read when the kernel runs.  Where
+ *           it is NaN the step is left out: nothing is written.
+ * 0 <= b1, b2 < 1; 0 <= eps; step >= 1.
+ */
+#define RESBM_TYPE_F32   0
+#define RESBM_TYPE_BF16  1
+#define RESBM_STATE_F32  0
+#define RESBM_STATE_E4M3 1
+typedef struct {
+  int64_t numel;
+  float* p;
+  const void* g;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  void* copy;
+  int32_t g_type;
+  int32_t state;
+  float weight_decay;
+  int32_t reserved;
+} resbm_adamw_tensor;
+size_t resbm_adamw_plan_bytes(const resbm_adamw_tensor* tensors, int64_t count);
+int32_t resbm_adamw_plan(const resbm_adamw_tensor* tensors, int64_t count, void* plan, size_t plan_bytes);
+int32_t resbm_adamw_update(const void* plan, const void* plan_dev, double lr, double beta1, double beta2,
+                           double eps, int64_t step, const double* lr_step, const float* grad_scale,
+                           void* stream);
+
+/*
+ * The 2-norm of all gradients of a plan and the factor that clips it:
+ *     out[0] = sqrt(sum g^2),   out[1] = min(1, max_norm / (norm + 1e-6))
+ * (float64 sums in a fixed order, rounded once; max_norm > 0).  out[1] is NaN
+ * where the norm is not finite, so that resbm_adamw_update with
+ * grad_scale = out + 1 leaves such a step out.
+ *  out  device array of two float32.
+ *  ws   at least resbm_grad_norm_workspace_bytes(plan) bytes, 256-byte aligned.
+ */
+size_t resbm_grad_norm_workspace_bytes(const void* plan);
+int32_t resbm_grad_norm(const void* plan, const void* plan_dev, double max_norm, float* out,
+                        void* ws, size_t ws_bytes, void* stream);
 
 /* RESBM_IO_BF16 for libresbm.so, RESBM_IO_F32 for the validation build. */
 int32_t resbm_io_dtype(void);

@@ -1,0 +1,468 @@
+// resbm_adamw.hpp -- one AdamW step, and the gradients' norm, over many tensors at once, gfx950.
+//
+// Muon (resbm_muon_update) takes a stage's bottleneck weights; gains, projections and embeddings take
+//     m <- b1 m + (1 - b1) g,   v <- b2 v + (1 - b2) g^2,
+//     p <- p (1 - lr wd) - (lr / c1) m / (sqrt(v) / sqrt(c2) + eps),   ck = 1 - bk^step,
+// element by element on 16 to 30 bytes an element and some 15 operations, so HBM bounds it, and launch
+// latency where the tensors are small.  One launch therefore covers all tensors: a plan in device memory
+// lists them and, for every chunk of kChunk elements, the tensor that it belongs to.  A block takes a chunk
+// at a time; a lane takes four consecutive elements, 16 bytes of every float32 array.
+// Arithmetic is float32 in the order written above, every operation rounded once (no contraction), so that
+// results do not depend on the form a tensor is listed in.
+//
+// States in 8 bits: blocks of 256 elements, counted from the tensor's start, hold m and u = sqrt(v) as e4m3
+// with one float32 scale each, s = max(amax (1 / 448), 2^-126).  A block is the 256 elements that a wave takes at
+// once, so its maximum is one reduction over lanes.  u rather than v, because the square root halves the
+// exponent's range: 2^-9 .. 448 covers u over five decades, v over ten.  A non-zero u never becomes zero (it
+// rounds up to the smallest code): |m| is at most a few u, so m / u stays bounded where u is small beside
+// the block's largest, while m / (0 + eps) would not.  The step itself uses the new m and v before their rounding.
+// Included by resbm_matrix.hip.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <stdlib.h>
+#include <string.h>
+
+#include <algorithm>
+
+#include "resbm.h"
+#include "resbm_host.hpp"
+#include "resbm_norm.hpp"
+
+namespace resbm_aw {
+
+using resbm_nm::e4m3_scale;
+using resbm_nm::mag;
+using resbm_nm::to_e4m3;
+using resbm_nm::umax;
+using resbm_nm::wave_max;
+
+constexpr int kBlock = 256;            // elements per scale of an 8-bit state: 64 lanes x 4
+constexpr int kThreads = 256;
+constexpr int kTurns = 2;              // a wave's turns per chunk
+constexpr int kChunk = kThreads * 4 * kTurns;
+constexpr int64_t kMaxBlocks = 1 << 20;
+constexpr int kNormBlocks = 2048;      // partial sums of the norm
+constexpr uint32_t kMagic = 0x57414452u;
+
+// The plan, in host and device memory alike: Head, Entry[count], uint32 tensor[chunks].
+struct Entry {
+  float* p;
+  const void* g;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  __bf16* copy;
+  int64_t numel, first;  // first: the tensor's first chunk
+  float wd;
+  int32_t g16, q8, vec;  // vec: every pointer allows 16-byte (bf16: 8, codes: 4) access
+};
+struct Head {
+  uint32_t magic, grads_only;
+  int64_t count, chunks, bytes;
+};
+static_assert(sizeof(Head) == 32 && sizeof(Entry) == 88, "plan layout");
+
+struct Table {
+  const Entry* entry;
+  const uint32_t* tensor;
+};
+
+struct Hyper {
+  double lr, b1, b2;
+  float fb1, fb2, ob1, ob2, eps;  // bk and 1 - bk in float32
+  float rate, rc2;                // lr / c1 and 1 / sqrt(c2)
+  const double* lr_step;
+  const float* grad_scale;
+};
+
+typedef float f2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ void from_e4m3(uint32_t q, float (&f)[4]) {
+  const f2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)q, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)q, true);
+  f[0] = a.x, f[1] = a.y, f[2] = b.x, f[3] = b.y;
+}
+
+// Four elements from e on, of which `left` exist; those beyond are zero.
+__device__ __forceinline__ void load_f32(const float* p, int64_t e, int left, bool vec, float (&f)[4]) {
+  if (vec && left >= 4) {
+    const float4 v = *(const float4*)(p + e);
+    f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = i < left ? p[e + i] : 0.0f;
+}
+__device__ __forceinline__ void store_f32(float* p, int64_t e, int left, bool vec, const float (&f)[4]) {
+  if (vec && left >= 4) {
+    *(float4*)(p + e) = make_float4(f[0], f[1], f[2], f[3]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < left) p[e + i] = f[i];
+}
+__device__ __forceinline__ void load_grad(const Entry& t, int64_t e, int left, bool vec, float (&f)[4]) {
+  if (!t.g16) return load_f32((const float*)t.g, e, left, vec, f);
+  const uint16_t* g = (const uint16_t*)t.g;
+  if (vec && left >= 4) {
+    const uint2 v = *(const uint2*)(g + e);
+    f[0] = __builtin_bit_cast(float, v.x << 16), f[1] = __builtin_bit_cast(float, v.x & 0xFFFF0000u);
+    f[2] = __builtin_bit_cast(float, v.y << 16), f[3] = __builtin_bit_cast(float, v.y & 0xFFFF0000u);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = i < left ? __builtin_bit_cast(float, (uint32_t)g[e + i] << 16) : 0.0f;
+}
+__device__ __forceinline__ uint32_t load_codes(const void* p, int64_t e, int left, bool vec) {
+  const uint8_t* q = (const uint8_t*)p + e;
+  if (vec && left >= 4) return *(const uint32_t*)q;
+  uint32_t v = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < left) v |= (uint32_t)q[i] << (8 * i);
+  return v;
+}
+__device__ __forceinline__ void store_codes(void* p, int64_t e, int left, bool vec, uint32_t v) {
+  uint8_t* q = (uint8_t*)p + e;
+  if (vec && left >= 4) {
+    *(uint32_t*)q = v;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < left) q[i] = (uint8_t)(v >> (8 * i));
+}
+__device__ __forceinline__ void store_copy(__bf16* p, int64_t e, int left, bool vec, const float (&f)[4]) {
+  typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+  const b4 v = {(__bf16)f[0], (__bf16)f[1], (__bf16)f[2], (__bf16)f[3]};
+  if (vec && left >= 4) {
+    *(b4*)(p + e) = v;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < left) p[e + i] = v[i];
+}
+
+// b^n by squaring, in float64: the bias correction of a step that only the device knows.
+__device__ __forceinline__ double power(double b, uint64_t n) {
+  double r = 1.0;
+  for (; n; n >>= 1) {
+    if (n & 1) r *= b;
+    b *= b;
+  }
+  return r;
+}
+
+__global__ __launch_bounds__(kThreads) void k_adamw(Table tab, int64_t chunks, Hyper hy) {
+#pragma clang fp contract(off)
+  float gs = 1.0f;
+  if (hy.grad_scale) {
+    gs = *hy.grad_scale;
+    if (gs != gs) return;  // no norm, no step: everything stays as it is
+  }
+  double lr = hy.lr;
+  float rate = hy.rate, rc2 = hy.rc2;
+  if (hy.lr_step) {
+    lr = hy.lr_step[0];
+    const double step = hy.lr_step[1];
+    const uint64_t n = step >= 1.0 ? (step < 1e18 ? (uint64_t)step : (uint64_t)1e18) : 1;
+    rate = (float)(lr / (1.0 - power(hy.b1, n)));
+    rc2 = (float)(1.0 / sqrt(1.0 - power(hy.b2, n)));
+  }
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+    const Entry t = tab.entry[tab.tensor[c]];
+    const float keep = (float)(1.0 - lr * (double)t.wd);
+    const bool vec = t.vec;
+#pragma unroll
+    for (int k = 0; k < kTurns; ++k) {
+      const int64_t w0 = (c - t.first) * kChunk + (k * (kThreads / 64) + wave) * kBlock;  // the wave's 256 elements
+      if (w0 >= t.numel) break;
+      const int64_t e = w0 + lane * 4, rest = t.numel - e;
+      const int left = rest < 0 ? 0 : rest > 4 ? 4 : (int)rest;
+      float p[4], g[4], m[4], v[4], u[4];
+      load_f32(t.p, e, left, vec, p);
+      load_grad(t, e, left, vec, g);
+      if (t.q8) {
+        const float ms = t.m_scale[w0 / kBlock], us = t.v_scale[w0 / kBlock];
+        from_e4m3(load_codes(t.m, e, left, vec), m);
+        from_e4m3(load_codes(t.v, e, left, vec), v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          m[i] = m[i] * ms;
+          v[i] = v[i] * us;
+          v[i] = v[i] * v[i];
+          if (i >= left) m[i] = v[i] = 0.0f;
+        }
+      } else {
+        load_f32((const float*)t.m, e, left, vec, m);
+        load_f32((const float*)t.v, e, left, vec, v);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (hy.grad_scale) g[i] = g[i] * gs;
+        m[i] = m[i] * hy.fb1 + g[i] * hy.ob1;
+        v[i] = v[i] * hy.fb2 + g[i] * hy.ob2 * g[i];
+        u[i] = sqrtf(v[i]);
+        p[i] = p[i] * keep - m[i] / (u[i] * rc2 + hy.eps) * rate;
+      }
+      store_f32(t.p, e, left, vec, p);
+      if (t.copy) store_copy(t.copy, e, left, vec, p);
+      if (t.q8) {
+        uint32_t am = 0, au = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          am = umax(am, mag(m[i]));
+          au = umax(au, mag(u[i]));
+        }
+        const float ms = e4m3_scale(wave_max(am)), us = e4m3_scale(wave_max(au));
+        const float im = 1.0f / ms, iu = 1.0f / us;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          m[i] = m[i] * im;
+          const float q = u[i] * iu;
+          u[i] = u[i] > 0.0f && q < 0x1p-9f ? 0x1p-9f : q;
+        }
+        store_codes(t.m, e, left, vec, to_e4m3(m[0], m[1], m[2], m[3]));
+        store_codes(t.v, e, left, vec, to_e4m3(u[0], u[1], u[2], u[3]));
+        if (lane == 0) {
+          t.m_scale[w0 / kBlock] = ms;
+          t.v_scale[w0 / kBlock] = us;
+        }
+      } else {
+        store_f32((float*)t.m, e, left, vec, m);
+        store_f32((float*)t.v, e, left, vec, v);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- gradient norm
+// Sums are float64 from the first square on: any float32 gradient's square fits.
+__device__ __forceinline__ double block_sum(double v, double* lds) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double s = 0.0;
+  for (int i = 0; i < (int)(blockDim.x >> 6); ++i) s += lds[i];
+  return s;
+}
+
+__global__ __launch_bounds__(kThreads) void k_grad_norm(Table tab, int64_t chunks, double* part) {
+  __shared__ double s_red[kThreads / 64];
+  double s = 0.0;
+  for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+    const Entry t = tab.entry[tab.tensor[c]];
+#pragma unroll
+    for (int k = 0; k < kTurns; ++k) {
+      const int64_t e = (c - t.first) * kChunk + (k * kThreads + threadIdx.x) * 4, rest = t.numel - e;
+      const int left = rest < 0 ? 0 : rest > 4 ? 4 : (int)rest;
+      float g[4];
+      load_grad(t, e, left, t.vec, g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s = fma((double)g[i], (double)g[i], s);
+    }
+  }
+  s = block_sum(s, s_red);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(kThreads) void k_grad_norm_out(int parts, const double* part, double max_norm, float* out) {
+  __shared__ double s_red[kThreads / 64];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < parts; i += kThreads) s += part[i];
+  s = block_sum(s, s_red);
+  if (threadIdx.x == 0) {
+    const double norm = sqrt(s), f = max_norm / (norm + 1e-6);
+    out[0] = (float)norm;
+    out[1] = norm <= 1.7976931348623157e308 ? (float)(f < 1.0 ? f : 1.0) : __builtin_nanf("");
+  }
+}
+
+// ---------------------------------------------------------------- host
+using resbm_host::aligned;
+using resbm_host::launch_status;
+using resbm_host::overlap;
+
+inline int64_t chunks_of(int64_t numel) { return (numel + kChunk - 1) / kChunk; }
+inline size_t plan_size(int64_t count, int64_t chunks) {
+  return (sizeof(Head) + (size_t)count * sizeof(Entry) + (size_t)chunks * 4 + 255) & ~(size_t)255;
+}
+
+struct Range {
+  uintptr_t at, end;
+  int writes;
+};
+
+// The checks of a list; *chunks and *grads_only as the plan's head has them.
+inline int32_t check_list(const resbm_adamw_tensor* t, int64_t count, int64_t* chunks, bool* grads_only) {
+  if (count < 0 || count > (1 << 24)) return RESBM_E_SHAPE;
+  if (count > 0 && !t) return RESBM_E_NULL;
+  *chunks = 0;
+  int64_t bare = 0, work = 0;
+  for (int64_t i = 0; i < count; ++i) {
+    const resbm_adamw_tensor& a = t[i];
+    if (a.numel < 0 || a.numel > (int64_t)1 << 42) return RESBM_E_SHAPE;
+    if (a.g_type != RESBM_TYPE_F32 && a.g_type != RESBM_TYPE_BF16) return RESBM_E_KIND;
+    if (a.state != RESBM_STATE_F32 && a.state != RESBM_STATE_E4M3) return RESBM_E_KIND;
+    if (!(a.weight_decay >= 0.0f && a.weight_decay < 3.0e38f)) return RESBM_E_SHAPE;
+    const bool none = !a.p && !a.m && !a.v && !a.m_scale && !a.v_scale && !a.copy;
+    if (a.numel == 0) continue;
+    bare += none;
+    work += 1;
+    if (!a.g) return RESBM_E_NULL;
+    const bool q8 = a.state == RESBM_STATE_E4M3;
+    if (!none && (!a.p || !a.m || !a.v || (q8 && (!a.m_scale || !a.v_scale)))) return RESBM_E_NULL;
+    const size_t sg = a.g_type == RESBM_TYPE_BF16 ? 2 : 4, ss = q8 ? 1 : 4;
+    if (!aligned(a.p, 4) || !aligned(a.g, sg) || !aligned(a.m, ss) || !aligned(a.v, ss) || !aligned(a.copy, 2) ||
+        (q8 && (!aligned(a.m_scale, 4) || !aligned(a.v_scale, 4))))
+      return RESBM_E_ALIGN;
+    *chunks += chunks_of(a.numel);
+  }
+  if (*chunks > INT32_MAX) return RESBM_E_SHAPE;
+  if (bare != 0 && bare != work) return RESBM_E_NULL;  // all with parameters and states, or none
+  *grads_only = bare > 0;
+  return RESBM_OK;
+}
+
+// Nothing that a step writes may overlap anything else in the list: all ranges by address, and
+// the furthest end so far of those that are written, and of all, against the next one's start.
+inline int32_t check_overlap(const resbm_adamw_tensor* t, int64_t count) {
+  Range* r = (Range*)malloc((size_t)count * 7 * sizeof(Range) + 1);
+  if (!r) return RESBM_E_WORKSPACE;
+  size_t k = 0;
+  for (int64_t i = 0; i < count; ++i) {
+    const resbm_adamw_tensor& a = t[i];
+    const bool q8 = a.state == RESBM_STATE_E4M3;
+    const size_t n = (size_t)a.numel, nb = (n + kBlock - 1) / kBlock * 4;
+    const auto put = [&](const void* p, size_t bytes, int writes) {
+      if (p && bytes) r[k++] = {(uintptr_t)p, (uintptr_t)p + bytes, writes};
+    };
+    put(a.p, n * 4, 1);
+    put(a.g, n * (a.g_type == RESBM_TYPE_BF16 ? 2 : 4), 0);
+    put(a.m, n * (q8 ? 1 : 4), 1);
+    put(a.v, n * (q8 ? 1 : 4), 1);
+    put(q8 ? a.m_scale : nullptr, nb, 1);
+    put(q8 ? a.v_scale : nullptr, nb, 1);
+    put(a.copy, n * 2, 1);
+  }
+  std::sort(r, r + k, [](const Range& a, const Range& b) { return a.at < b.at; });
+  uintptr_t written = 0, any = 0;
+  bool clash = false;
+  for (size_t i = 0; i < k && !clash; ++i) {
+    clash = r[i].at < (r[i].writes ? any : written);
+    any = r[i].end > any ? r[i].end : any;
+    if (r[i].writes) written = r[i].end > written ? r[i].end : written;
+  }
+  free(r);
+  return clash ? RESBM_E_ALIAS : RESBM_OK;
+}
+
+// The head of the host's copy, if it is a plan.
+inline const Head* head_of(const void* plan) {
+  const Head* h = (const Head*)plan;
+  return h && aligned(plan, 8) && h->magic == kMagic ? h : nullptr;
+}
+inline Table table_of(const Head* h, const void* dev) {
+  const char* d = (const char*)dev;
+  return {(const Entry*)(d + sizeof(Head)), (const uint32_t*)(d + sizeof(Head) + h->count * sizeof(Entry))};
+}
+inline int norm_blocks(int64_t chunks) { return (int)(chunks < kNormBlocks ? chunks : kNormBlocks); }
+
+}  // namespace resbm_aw
+
+extern "C" {
+
+size_t resbm_adamw_plan_bytes(const resbm_adamw_tensor* tensors, int64_t count) {
+  int64_t chunks;
+  bool grads_only;
+  if (resbm_aw::check_list(tensors, count, &chunks, &grads_only) != RESBM_OK) return 0;
+  return resbm_aw::plan_size(count, chunks);
+}
+
+int32_t resbm_adamw_plan(const resbm_adamw_tensor* tensors, int64_t count, void* plan, size_t plan_bytes) {
+  using namespace resbm_aw;
+  int64_t chunks;
+  bool grads_only;
+  int32_t st = check_list(tensors, count, &chunks, &grads_only);
+  if (st != RESBM_OK) return st;
+  if (!plan) return RESBM_E_NULL;
+  if (!aligned(plan, 8)) return RESBM_E_ALIGN;
+  const size_t bytes = plan_size(count, chunks);
+  if (plan_bytes < bytes) return RESBM_E_WORKSPACE;
+  st = check_overlap(tensors, count);
+  if (st != RESBM_OK) return st;
+  memset(plan, 0, bytes);
+  Head* h = (Head*)plan;
+  Entry* e = (Entry*)((char*)plan + sizeof(Head));
+  uint32_t* at = (uint32_t*)(e + count);
+  int64_t c = 0;
+  for (int64_t i = 0; i < count; ++i) {
+    const resbm_adamw_tensor& a = tensors[i];
+    const bool q8 = a.state == RESBM_STATE_E4M3, g16 = a.g_type == RESBM_TYPE_BF16;
+    e[i] = {a.p, a.g, a.m, a.v, a.m_scale, a.v_scale, (__bf16*)a.copy, a.numel, c, a.weight_decay, g16, q8,
+            aligned(a.p, 16) && aligned(a.g, g16 ? 8 : 16) && aligned(a.m, q8 ? 4 : 16) && aligned(a.v, q8 ? 4 : 16) &&
+                aligned(a.copy, 8)};
+    for (int64_t k = chunks_of(a.numel); k > 0; --k) at[c++] = (uint32_t)i;
+  }
+  h->grads_only = grads_only;
+  h->count = count;
+  h->chunks = chunks;
+  h->bytes = (int64_t)bytes;
+  h->magic = kMagic;
+  return RESBM_OK;
+}
+
+int32_t resbm_adamw_update(const void* plan, const void* plan_dev, double lr, double beta1, double beta2, double eps,
+                           int64_t step, const double* lr_step, const float* grad_scale, void* stream) {
+  using namespace resbm_aw;
+  if (!plan) return RESBM_E_NULL;
+  const Head* h = head_of(plan);
+  if (!h) return RESBM_E_KIND;
+  if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0 && eps < 3.0e38)) return RESBM_E_SHAPE;
+  if (!lr_step && (step < 1 || !isfinite(lr))) return RESBM_E_SHAPE;
+  if (h->chunks == 0) return RESBM_OK;
+  if (!plan_dev || h->grads_only) return RESBM_E_NULL;
+  if (!aligned(plan_dev, 256) || !aligned(lr_step, 8) || !aligned(grad_scale, 4)) return RESBM_E_ALIGN;
+  const double n = (double)(lr_step ? 1 : step);
+  const Hyper hy = {lr, beta1, beta2, (float)beta1, (float)beta2, (float)(1.0 - beta1), (float)(1.0 - beta2), (float)eps,
+                    (float)(lr / (1.0 - pow(beta1, n))), (float)(1.0 / sqrt(1.0 - pow(beta2, n))), lr_step, grad_scale};
+  const int64_t blocks = h->chunks < kMaxBlocks ? h->chunks : kMaxBlocks;
+  hipLaunchKernelGGL(k_adamw, dim3((uint32_t)blocks), dim3(kThreads), 0, (hipStream_t)stream, table_of(h, plan_dev),
+                     h->chunks, hy);
+  return launch_status();
+}
+
+size_t resbm_grad_norm_workspace_bytes(const void* plan) {
+  using namespace resbm_aw;
+  const Head* h = head_of(plan);
+  return h ? ((size_t)norm_blocks(h->chunks) * 8 + 256) & ~(size_t)255 : 0;
+}
+
+int32_t resbm_grad_norm(const void* plan, const void* plan_dev, double max_norm, float* out, void* ws, size_t ws_bytes,
+                        void* stream) {
+  using namespace resbm_aw;
+  if (!plan) return RESBM_E_NULL;
+  const Head* h = head_of(plan);
+  if (!h) return RESBM_E_KIND;
+  if (!(max_norm > 0.0)) return RESBM_E_SHAPE;
+  if (!out || !ws || (!plan_dev && h->chunks > 0)) return RESBM_E_NULL;
+  if (!aligned(plan_dev, 256) || !aligned(out, 4) || !aligned(ws, 256)) return RESBM_E_ALIGN;
+  const size_t need = resbm_grad_norm_workspace_bytes(plan);
+  if (ws_bytes < need) return RESBM_E_WORKSPACE;
+  if (overlap(out, 8, ws, need) || overlap(out, 8, plan_dev, h->bytes) || overlap(ws, need, plan_dev, h->bytes))
+    return RESBM_E_ALIAS;
+  const Table tab = table_of(h, plan_dev);
+  const int parts = norm_blocks(h->chunks);
+  if (parts > 0)
+    hipLaunchKernelGGL(k_grad_norm, dim3(parts), dim3(kThreads), 0, (hipStream_t)stream, tab, h->chunks, (double*)ws);
+  hipLaunchKernelGGL(k_grad_norm_out, dim3(1), dim3(kThreads), 0, (hipStream_t)stream, parts, (const double*)ws, max_norm,
+                     out);
+  return launch_status();
+}
+
+}  // extern "C"

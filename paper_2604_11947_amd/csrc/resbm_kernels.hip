@@ -2760,6 +2760,7 @@ const char* resbm_strerror(int32_t status) {
     case RESBM_E_ACT: return "unknown activation, or SiLU backward without a_save";
     case RESBM_E_HIP: return "a HIP kernel launch failed";
     case RESBM_E_ALIAS: return "an output overlaps an input it may not alias";
+    case RESBM_E_KIND: return "unknown element type or state form, or not a plan";
     default: return "unknown status";
   }
 }

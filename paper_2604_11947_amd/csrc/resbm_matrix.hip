@@ -50,6 +50,11 @@
 #include "resbm.h"
 #include "resbm_host.hpp"
 
+// The operators next to the boundary that are no contractions, in namespaces of their
+// own: the residual norm, and the optimizer step of the tensors that Muon does not take.
+#include "resbm_norm.hpp"
+#include "resbm_adamw.hpp"
+
 namespace resbm_mx {
 
 constexpr int kThreads = 256;

@@ -38,6 +38,13 @@ E_WORKSPACE = -4
 E_ACT = -5
 E_HIP = -6
 E_ALIAS = -7
+E_KIND = -8
+
+TYPE_F32 = 0
+TYPE_BF16 = 1
+STATE_F32 = 0
+STATE_E4M3 = 1
+STATE_BLOCK = 256  # elements per scale of an 8-bit state
 
 # Newton-Schulz coefficients of the Muon method the paper cites (Sec. 3.4)
 NS_QUINTIC = (3.4445, -4.7750, 2.0315)
@@ -70,6 +77,17 @@ SIGNATURES = [
     ("resbm_ffn_encode_workspace_bytes", _sz, [_i64, _i32, _i32]),
     ("resbm_decode_qkv_fwd", _i32, [_i64, _i32, _i32, _i32, _p, _p, _p, _p, ctypes.c_float, _p, _i64, _p, _sz, _p]),
     ("resbm_decode_qkv_workspace_bytes", _sz, [_i32, _i32]),
+    ("resbm_skip_norm_fwd", _i32, [_i64, _i32, _i32, _p, _i64, _p, _i64, _p, _p, ctypes.c_float, _p, _i64, _p, _i64, _p,
+                                   _p]),
+    ("resbm_skip_norm_q8_fwd", _i32, [_i64, _i32, _i32, _i32, _p, _i64, _p, _i64, _p, _p, ctypes.c_float, _p, _i64, _p,
+                                      _i64, _p, _p, _p]),
+    ("resbm_skip_norm_bwd", _i32, [_i64, _i32, _p, _i64, _p, _p, _p, _i64, _p, _i64, _p, _i64, _p, _i32, _p, _sz, _p]),
+    ("resbm_norm_workspace_bytes", _sz, [_i64, _i32]),
+    ("resbm_adamw_plan_bytes", _sz, [_p, _i64]),
+    ("resbm_adamw_plan", _i32, [_p, _i64, _p, _sz]),
+    ("resbm_adamw_update", _i32, [_p, _p, _d, _d, _d, _d, _i64, _p, _p, _p]),
+    ("resbm_grad_norm_workspace_bytes", _sz, [_p]),
+    ("resbm_grad_norm", _i32, [_p, _p, _d, _p, _p, _sz, _p]),
     ("resbm_io_dtype", _i32, []),
     ("resbm_strerror", ctypes.c_char_p, [_i32]),
 ]
@@ -107,10 +125,40 @@ def _dtype(t, dtype, name):
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
 
 
-def _stream(stream, ref: torch.Tensor):
+def _vector(t: torch.Tensor, size: int, name: str) -> None:
+    _dtype(t, torch.float32, name)
+    if t.dim() != 1 or t.numel() != size or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous vector of {size} elements, got {tuple(t.shape)}")
+
+
+def _grad_dtype(t: torch.Tensor, i: int) -> None:
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"g[{i}]: expected torch.float32 or torch.bfloat16, got {t.dtype}")
+
+
+def _stream(stream, ref):
     if stream is None:
         stream = torch.cuda.current_stream(ref.device)
     return ctypes.c_void_p(getattr(stream, "cuda_stream", stream))
+
+
+class AdamWTensor(ctypes.Structure):
+    """resbm_adamw_tensor."""
+    _fields_ = [("numel", ctypes.c_int64)] + [(k, ctypes.c_void_p) for k in ("p", "g", "m", "v", "m_scale", "v_scale",
+                                                                             "copy")] + [
+        ("g_type", ctypes.c_int32), ("state", ctypes.c_int32), ("weight_decay", ctypes.c_float),
+        ("reserved", ctypes.c_int32)]
+
+
+class AdamWPlan:
+    """A plan's host and device copies, and the tensors whose addresses it holds.
+
+    Made by ``Library.adamw_plan`` or ``Library.grad_plan`` with the tensors' current
+    addresses; a tensor that moves needs a new plan."""
+
+    def __init__(self, host, device_table, tensors, device):
+        self.host, self.table, self.tensors, self.device = host, device_table, tensors, device
+        self.host_ptr, self.table_ptr = ctypes.addressof(host), device_table.data_ptr()
 
 
 class Library:
@@ -474,6 +522,155 @@ class Library:
         st = self.cdll.resbm_spectrum(p, q, _ptr(W), _ptr(sigma), _ptr(r_eff), _ptr(ws), ws.numel(),
                                       _stream(stream, W))
         self._check("resbm_spectrum", st)
+
+    # ------------------------------------------------------------ residual addition and RMS norm
+    def norm_workspace(self, T: int, n: int, device) -> torch.Tensor:
+        return self._buffer(int(self.cdll.resbm_norm_workspace_bytes(T, n)), device)
+
+    @staticmethod
+    def _buffer(nbytes: int, device) -> torch.Tensor:
+        buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=device)
+        return buf[(-buf.data_ptr()) % 256:][:nbytes]
+
+    def _norm_inputs(self, x, gamma, res, b, h, rstd):
+        """Checks what the two forward norms share; (T, n, r, ld_x, ld_res, ld_h)."""
+        T, n = x.shape
+        for t, nm in ((x, "x"), (res, "res"), (b, "b"), (h, "h")):
+            _dtype(t, self.io_dtype, nm)
+        _vector(gamma, n, "gamma")
+        if rstd is not None:
+            _vector(rstd, T, "rstd")
+        r = 0
+        if b is not None:
+            r = b.shape[1] if b.dim() == 2 else -1
+            _packed(b, T, r, "b")
+        return (T, n, r, _ld(x, T, n, "x"), 0 if res is None else _ld(res, T, n, "res"),
+                0 if h is None else _ld(h, T, n, "h"))
+
+    def skip_norm_fwd(self, x, gamma, y, res=None, b=None, h=None, rstd=None, eps=1e-5, stream=None):
+        """h = x + res + b I (rounded once; written when ``h`` is given), y = RMSNorm(h) gamma."""
+        T, n, r, ld_x, ld_res, ld_h = self._norm_inputs(x, gamma, res, b, h, rstd)
+        _dtype(y, self.io_dtype, "y")
+        ld_y = _ld(y, T, n, "y")
+        st = self.cdll.resbm_skip_norm_fwd(T, n, r, _ptr(x), ld_x, _ptr(res), ld_res, _ptr(b), _ptr(gamma), eps, _ptr(h),
+                                           ld_h, _ptr(y), ld_y, _ptr(rstd), _stream(stream, x))
+        self._check("resbm_skip_norm_fwd", st)
+
+    def skip_norm_q8_fwd(self, x, gamma, y, scale, res=None, b=None, h=None, rstd=None, eps=1e-5, stream=None):
+        """skip_norm_fwd with y in e4m3 and float32 scales; ``scale`` (T, n / group) sets the group of columns."""
+        T, n, r, ld_x, ld_res, ld_h = self._norm_inputs(x, gamma, res, b, h, rstd)
+        _dtype(y, torch.float8_e4m3fn, "y")
+        _dtype(scale, torch.float32, "scale")
+        ld_y = _ld(y, T, n, "y")
+        groups = scale.shape[1] if scale.dim() == 2 else 0
+        if groups < 1 or n % groups:
+            raise ValueError(f"scale: expected shape ({T}, n / group), got {tuple(scale.shape)}")
+        _packed(scale, T, groups, "scale")
+        st = self.cdll.resbm_skip_norm_q8_fwd(T, n, r, n // groups, _ptr(x), ld_x, _ptr(res), ld_res, _ptr(b),
+                                              _ptr(gamma), eps, _ptr(h), ld_h, _ptr(y), ld_y, _ptr(scale), _ptr(rstd),
+                                              _stream(stream, x))
+        self._check("resbm_skip_norm_q8_fwd", st)
+
+    def skip_norm_bwd(self, h, gamma, rstd, g_y, g_x, dgamma, g_h=None, accumulate=False, ws=None, stream=None):
+        """The norm's gradient plus g_h in g_x (which may be g_y or g_h), the gain's in dgamma."""
+        T, n = h.shape
+        for t, nm in ((h, "h"), (g_y, "g_y"), (g_h, "g_h"), (g_x, "g_x")):
+            _dtype(t, self.io_dtype, nm)
+        _vector(gamma, n, "gamma")
+        _vector(rstd, T, "rstd")
+        _vector(dgamma, n, "dgamma")
+        ld_h, ld_gy, ld_gx = _ld(h, T, n, "h"), _ld(g_y, T, n, "g_y"), _ld(g_x, T, n, "g_x")
+        ld_gh = _ld(g_h, T, n, "g_h") if g_h is not None else 0
+        if ws is None:
+            ws = self.norm_workspace(T, n, h.device)
+        st = self.cdll.resbm_skip_norm_bwd(T, n, _ptr(h), ld_h, _ptr(gamma), _ptr(rstd), _ptr(g_y), ld_gy, _ptr(g_h),
+                                           ld_gh, _ptr(g_x), ld_gx, _ptr(dgamma), int(bool(accumulate)), _ptr(ws),
+                                           ws.numel(), _stream(stream, h))
+        self._check("resbm_skip_norm_bwd", st)
+
+    # ------------------------------------------------------------ AdamW over many tensors
+    def adamw_plan(self, p, g, m, v, m_scale=None, v_scale=None, copy=None, weight_decay=0.0) -> AdamWPlan:
+        """The plan of the lists' tensors: float32 ``p``, gradients float32 or bf16, states float32 or, with
+        ``m_scale`` and ``v_scale`` (an entry may be None), float8_e4m3fn; ``copy``: bf16 tensors or None."""
+        k = len(p)
+        none = [None] * k
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * k
+        lists = [list(t) if t is not None else none for t in (p, g, m, v, m_scale, v_scale, copy)]
+        if any(len(t) != k for t in lists + [decay]):
+            raise ValueError("adamw_plan: lists of different lengths")
+        entries = (AdamWTensor * max(k, 1))()
+        for i, (e, wd, row) in enumerate(zip(entries, decay, zip(*lists))):
+            P, G, M, V, ms, vs, cp = row
+            q8 = ms is not None
+            _dtype(P, torch.float32, f"p[{i}]")
+            _grad_dtype(G, i)
+            for t, nm in ((M, "m"), (V, "v")):
+                _dtype(t, torch.float8_e4m3fn if q8 else torch.float32, f"{nm}[{i}]")
+            _dtype(cp, torch.bfloat16, f"copy[{i}]")
+            if (vs is not None) != q8:
+                raise ValueError(f"m_scale[{i}], v_scale[{i}]: both or neither")
+            for t, nm in ((P, "p"), (G, "g"), (M, "m"), (V, "v"), (cp, "copy")):
+                if t is not None and (t.numel() != P.numel() or not t.is_contiguous()):
+                    raise ValueError(f"{nm}[{i}]: expected a contiguous tensor of {P.numel()} elements")
+            for t, nm in ((ms, "m_scale"), (vs, "v_scale")):
+                if t is not None:
+                    _vector(t, -(-P.numel() // STATE_BLOCK), f"{nm}[{i}]")
+            e.numel, e.weight_decay = P.numel(), wd
+            e.g_type, e.state = TYPE_BF16 if G.dtype == torch.bfloat16 else TYPE_F32, STATE_E4M3 if q8 else STATE_F32
+            for name, t in zip(("p", "g", "m", "v", "m_scale", "v_scale", "copy"), row):
+                setattr(e, name, None if t is None else t.data_ptr())
+        return self._plan(entries, k, lists)
+
+    def grad_plan(self, g) -> AdamWPlan:
+        """A plan of gradients alone, for grad_norm."""
+        entries = (AdamWTensor * max(len(g), 1))()
+        for i, (e, G) in enumerate(zip(entries, g)):
+            _grad_dtype(G, i)
+            if not G.is_contiguous():
+                raise ValueError(f"g[{i}]: expected a contiguous tensor")
+            e.numel, e.g, e.g_type = G.numel(), G.data_ptr(), TYPE_BF16 if G.dtype == torch.bfloat16 else TYPE_F32
+        return self._plan(entries, len(g), [list(g)])
+
+    def _plan(self, entries, count, lists) -> AdamWPlan:
+        tensors = [t for row in lists for t in row if t is not None]
+        devices = {t.device for t in tensors}
+        if len(devices) > 1 or any(d.type != "cuda" for d in devices):
+            raise ValueError(f"a plan's tensors are on one GPU, got {sorted(map(str, devices))}")
+        device = devices.pop() if devices else torch.device("cuda", torch.cuda.current_device())
+        nbytes = int(self.cdll.resbm_adamw_plan_bytes(entries, count))
+        host = (ctypes.c_int64 * (max(nbytes, 256) // 8))()
+        self._check("resbm_adamw_plan", self.cdll.resbm_adamw_plan(entries, count, host, nbytes))
+        table = self._buffer(nbytes, device)
+        table.copy_(torch.frombuffer(host, dtype=torch.uint8)[:nbytes])
+        return AdamWPlan(host, table, tensors, device)
+
+    def adamw_update(self, plan: AdamWPlan, lr=0.0, step=1, betas=(0.9, 0.95), eps=1e-8, grad_scale=None, lr_step=None,
+                     stream=None):
+        """One AdamW step on the plan's tensors.  ``grad_scale``: a float32 tensor of one element on the device, the
+        gradients' factor (NaN leaves the step out); ``lr_step``: a float64 tensor {lr, step} there, read when the
+        kernel runs, in place of ``lr`` and ``step``."""
+        for t, dt, k, nm in ((grad_scale, torch.float32, 1, "grad_scale"), (lr_step, torch.float64, 2, "lr_step")):
+            if t is not None:
+                _dtype(t, dt, nm)
+                if t.numel() != k or not t.is_contiguous() or t.device != plan.device:
+                    raise ValueError(f"{nm}: expected {k} contiguous elements on {plan.device}")
+        st = self.cdll.resbm_adamw_update(plan.host_ptr, plan.table_ptr, lr, betas[0], betas[1], eps, step,
+                                          _ptr(lr_step), _ptr(grad_scale), _stream(stream, plan))
+        self._check("resbm_adamw_update", st)
+
+    def grad_norm_workspace(self, plan: AdamWPlan) -> torch.Tensor:
+        return self._buffer(int(self.cdll.resbm_grad_norm_workspace_bytes(plan.host_ptr)), plan.device)
+
+    def grad_norm(self, plan: AdamWPlan, max_norm, out, ws=None, stream=None):
+        """out[0] = the 2-norm of the plan's gradients, out[1] = min(1, max_norm / norm): adamw_update's grad_scale."""
+        _vector(out, 2, "out")
+        if out.device != plan.device:
+            raise ValueError(f"out: expected a tensor on {plan.device}")
+        if ws is None:
+            ws = self.grad_norm_workspace(plan)
+        st = self.cdll.resbm_grad_norm(plan.host_ptr, plan.table_ptr, max_norm, _ptr(out), _ptr(ws), ws.numel(),
+                                       _stream(stream, plan))
+        self._check("resbm_grad_norm", st)
 
 
 _LOADED: dict[str, Library] = {}
