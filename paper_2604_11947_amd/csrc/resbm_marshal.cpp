@@ -236,6 +236,139 @@ PyObject* muon_update(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+void* vector(PyObject* o, int64_t size) {
+  const at::Tensor& v = tensor(o, F32);
+  need(v.dim() == 1 && v.size(0) == size && v.is_contiguous());
+  return v.data_ptr();
+}
+void* vector_or_none(PyObject* o, int64_t size) { return o == Py_None ? nullptr : vector(o, size); }
+
+// What the two forward norms share, from a[1] on: (io_code, x, gamma, res, b, h, rstd, eps).
+struct NormIn {
+  int64_t T, n, r = 0, ld_x, ld_res, ld_h;
+  const void *x, *gamma, *res, *b = nullptr;
+  void *h, *rstd;
+  float eps;
+  at::ScalarType io;
+};
+NormIn norm_in(PyObject* const* a) {
+  NormIn v;
+  v.io = io_type(a[1]);
+  const at::Tensor& x = tensor(a[2], v.io);
+  need(x.dim() == 2);
+  v.T = x.size(0), v.n = x.size(1);
+  v.x = strided(a[2], v.io, v.T, v.n, &v.ld_x);
+  v.gamma = vector(a[3], v.n);
+  v.res = strided_or_none(a[4], v.io, v.T, v.n, &v.ld_res);
+  if (a[5] != Py_None) {
+    const at::Tensor& b = tensor(a[5], v.io);
+    need(b.dim() == 2);
+    v.r = b.size(1);
+    v.b = packed(a[5], v.io, v.T, v.r);
+  }
+  v.h = strided_or_none(a[6], v.io, v.T, v.n, &v.ld_h);
+  v.rstd = vector_or_none(a[7], v.T);
+  v.eps = (float)real(a[8]);
+  return v;
+}
+
+typedef int32_t NormFwd(int64_t, int32_t, int32_t, const void*, int64_t, const void*, int64_t, const void*, const void*,
+                        float, void*, int64_t, void*, int64_t, void*, void*);
+typedef int32_t NormQ8(int64_t, int32_t, int32_t, int32_t, const void*, int64_t, const void*, int64_t, const void*,
+                       const void*, float, void*, int64_t, void*, int64_t, void*, void*, void*);
+typedef int32_t NormBwd(int64_t, int32_t, const void*, int64_t, const void*, const void*, const void*, int64_t,
+                        const void*, int64_t, void*, int64_t, void*, int32_t, void*, size_t, void*);
+typedef int32_t AdamW(const void*, const void*, double, double, double, double, int64_t, const void*, const void*, void*);
+typedef int32_t GradNorm(const void*, const void*, double, void*, void*, size_t, void*);
+
+// (fn, io_code, x, gamma, res, b, h, rstd, eps, y)
+PyObject* skip_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 10) Py_RETURN_NONE;
+  return guarded([&] {
+    const NormIn v = norm_in(a);
+    int64_t ld_y;
+    void* y = strided(a[9], v.io, v.T, v.n, &ld_y);
+    return call(a[0], (NormFwd*)nullptr, v.T, dim32(v.n), dim32(v.r), v.x, v.ld_x, v.res, v.ld_res, v.b, v.gamma, v.eps,
+                v.h, v.ld_h, y, ld_y, v.rstd, stream_of(THPVariable_Unpack(a[2])));
+  });
+}
+
+// (fn, io_code, x, gamma, res, b, h, rstd, eps, y, scale)
+PyObject* skip_norm_q8_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 11) Py_RETURN_NONE;
+  return guarded([&] {
+    const NormIn v = norm_in(a);
+    int64_t ld_y;
+    void* y = strided(a[9], at::kFloat8_e4m3fn, v.T, v.n, &ld_y);
+    const at::Tensor& sc = tensor(a[10], F32);
+    need(sc.dim() == 2 && sc.size(1) >= 1 && v.n % sc.size(1) == 0);
+    const int64_t groups = sc.size(1);
+    void* scale = packed(a[10], F32, v.T, groups);
+    return call(a[0], (NormQ8*)nullptr, v.T, dim32(v.n), dim32(v.r), dim32(v.n / groups), v.x, v.ld_x, v.res, v.ld_res,
+                v.b, v.gamma, v.eps, v.h, v.ld_h, y, ld_y, scale, v.rstd, stream_of(THPVariable_Unpack(a[2])));
+  });
+}
+
+// (fn, io_code, h, gamma, rstd, g_y, g_x, dgamma, g_h, accumulate, ws)
+PyObject* skip_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 11) Py_RETURN_NONE;
+  return guarded([&] {
+    const at::ScalarType io = io_type(a[1]);
+    const at::Tensor& h = tensor(a[2], io);
+    need(h.dim() == 2);
+    const int64_t T = h.size(0), nn = h.size(1);
+    int64_t ld_h, ld_gy, ld_gx, ld_gh;
+    const void* hp = strided(a[2], io, T, nn, &ld_h);
+    const void* ga = vector(a[3], nn);
+    const void* rs = vector(a[4], T);
+    const void* gy = strided(a[5], io, T, nn, &ld_gy);
+    void* gx = strided(a[6], io, T, nn, &ld_gx);
+    void* dg = vector(a[7], nn);
+    const void* gh = strided_or_none(a[8], io, T, nn, &ld_gh);
+    const int32_t acc = truth(a[9]);
+    const Bytes ws = workspace(a[10]);
+    return call(a[0], (NormBwd*)nullptr, T, dim32(nn), hp, ld_h, ga, rs, gy, ld_gy, gh, ld_gh, gx, ld_gx, dg, acc, ws.p,
+                ws.n, stream_of(h));
+  });
+}
+
+// A device array of `size` elements on the plan's device, or NULL for None.
+void* device_array(PyObject* o, at::ScalarType t, int64_t size, const at::Tensor& table) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& v = tensor(o, t);
+  need(v.numel() == size && v.is_contiguous() && v.get_device() == table.get_device());
+  return v.data_ptr();
+}
+
+// (fn, host plan's address, device plan, lr, step, (b1, b2), eps, grad_scale, lr_step)
+PyObject* adamw_update(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 9) Py_RETURN_NONE;
+  return guarded([&] {
+    const at::Tensor& table = tensor(a[2], at::kByte);
+    need(PyLong_CheckExact(a[4]) && PyTuple_CheckExact(a[5]) && PyTuple_GET_SIZE(a[5]) == 2);
+    int overflow = 0;
+    const int64_t step = PyLong_AsLongLongAndOverflow(a[4], &overflow);
+    need(!overflow);
+    const void* gs = device_array(a[7], F32, 1, table);
+    const void* ls = device_array(a[8], at::kDouble, 2, table);
+    return call(a[0], (AdamW*)nullptr, address(a[1]), table.data_ptr(), real(a[3]), real(PyTuple_GET_ITEM(a[5], 0)),
+                real(PyTuple_GET_ITEM(a[5], 1)), real(a[6]), step, ls, gs, stream_of(table));
+  });
+}
+
+// (fn, host plan's address, device plan, max_norm, out, ws)
+PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 6) Py_RETURN_NONE;
+  return guarded([&] {
+    const at::Tensor& table = tensor(a[2], at::kByte);
+    const at::Tensor& out = tensor(a[4], F32);
+    need(out.dim() == 1 && out.size(0) == 2 && out.is_contiguous() && out.get_device() == table.get_device());
+    const Bytes ws = workspace(a[5]);
+    return call(a[0], (GradNorm*)nullptr, address(a[1]), table.data_ptr(), real(a[3]), out.data_ptr(), ws.p, ws.n,
+                stream_of(table));
+  });
+}
+
 PyObject* init(PyObject*, PyObject* raw_stream) {
   Py_INCREF(raw_stream);
   Py_XDECREF(g_raw_stream);
@@ -245,6 +378,8 @@ PyObject* init(PyObject*, PyObject* raw_stream) {
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(encode_fwd), FAST(decode_fwd), FAST(decode_bwd), FAST(encode_bwd), FAST(muon_update),
+                         FAST(skip_norm_fwd), FAST(skip_norm_q8_fwd), FAST(skip_norm_bwd), FAST(adamw_update),
+                         FAST(grad_norm),
                          {"init", init, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

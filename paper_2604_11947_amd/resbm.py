@@ -549,6 +549,10 @@ class Library:
 
     def skip_norm_fwd(self, x, gamma, y, res=None, b=None, h=None, rstd=None, eps=1e-5, stream=None):
         """h = x + res + b I (rounded once; written when ``h`` is given), y = RMSNorm(h) gamma."""
+        if _marshal is not None and stream is None:
+            st = _marshal.skip_norm_fwd(self._at["resbm_skip_norm_fwd"], self.io_code, x, gamma, res, b, h, rstd, eps, y)
+            if st is not None:
+                return self._check("resbm_skip_norm_fwd", st)
         T, n, r, ld_x, ld_res, ld_h = self._norm_inputs(x, gamma, res, b, h, rstd)
         _dtype(y, self.io_dtype, "y")
         ld_y = _ld(y, T, n, "y")
@@ -558,6 +562,11 @@ class Library:
 
     def skip_norm_q8_fwd(self, x, gamma, y, scale, res=None, b=None, h=None, rstd=None, eps=1e-5, stream=None):
         """skip_norm_fwd with y in e4m3 and float32 scales; ``scale`` (T, n / group) sets the group of columns."""
+        if _marshal is not None and stream is None:
+            st = _marshal.skip_norm_q8_fwd(self._at["resbm_skip_norm_q8_fwd"], self.io_code, x, gamma, res, b, h, rstd,
+                                           eps, y, scale)
+            if st is not None:
+                return self._check("resbm_skip_norm_q8_fwd", st)
         T, n, r, ld_x, ld_res, ld_h = self._norm_inputs(x, gamma, res, b, h, rstd)
         _dtype(y, torch.float8_e4m3fn, "y")
         _dtype(scale, torch.float32, "scale")
@@ -573,6 +582,11 @@ class Library:
 
     def skip_norm_bwd(self, h, gamma, rstd, g_y, g_x, dgamma, g_h=None, accumulate=False, ws=None, stream=None):
         """The norm's gradient plus g_h in g_x (which may be g_y or g_h), the gain's in dgamma."""
+        if _marshal is not None and stream is None:
+            st = _marshal.skip_norm_bwd(self._at["resbm_skip_norm_bwd"], self.io_code, h, gamma, rstd, g_y, g_x, dgamma,
+                                        g_h, accumulate, ws)
+            if st is not None:
+                return self._check("resbm_skip_norm_bwd", st)
         T, n = h.shape
         for t, nm in ((h, "h"), (g_y, "g_y"), (g_h, "g_h"), (g_x, "g_x")):
             _dtype(t, self.io_dtype, nm)
@@ -649,6 +663,11 @@ class Library:
         """One AdamW step on the plan's tensors.  ``grad_scale``: a float32 tensor of one element on the device, the
         gradients' factor (NaN leaves the step out); ``lr_step``: a float64 tensor {lr, step} there, read when the
         kernel runs, in place of ``lr`` and ``step``."""
+        if _marshal is not None and stream is None:
+            st = _marshal.adamw_update(self._at["resbm_adamw_update"], plan.host_ptr, plan.table, lr, step, betas, eps,
+                                       grad_scale, lr_step)
+            if st is not None:
+                return self._check("resbm_adamw_update", st)
         for t, dt, k, nm in ((grad_scale, torch.float32, 1, "grad_scale"), (lr_step, torch.float64, 2, "lr_step")):
             if t is not None:
                 _dtype(t, dt, nm)
@@ -663,6 +682,10 @@ class Library:
 
     def grad_norm(self, plan: AdamWPlan, max_norm, out, ws=None, stream=None):
         """out[0] = the 2-norm of the plan's gradients, out[1] = min(1, max_norm / norm): adamw_update's grad_scale."""
+        if _marshal is not None and stream is None:
+            st = _marshal.grad_norm(self._at["resbm_grad_norm"], plan.host_ptr, plan.table, max_norm, out, ws)
+            if st is not None:
+                return self._check("resbm_grad_norm", st)
         _vector(out, 2, "out")
         if out.device != plan.device:
             raise ValueError(f"out: expected a tensor on {plan.device}")
