@@ -6,10 +6,14 @@
 // and backwards, with xh = h rstd, w = g_y gamma, c = mean_c(w xh),
 //     g_x = rstd (w - xh c) + g_h,   dgamma = sum_t g_y xh.
 // Every op reads each operand once and writes each result once, so HBM bounds them (about one
-// operation a byte); a row has to be whole before any of its results, so a team of TEAM lanes owns
-// a row and keeps it in registers: one wave for narrow rows, a block for wide ones.  The stream h is
-// rounded once, to the activations' type, and the norm is that of the rounded h, whether h is written
-// or not: then the backward pass, which reads h, is the adjoint of what the forward computed.
+// operation a byte).  A row has to be whole before any of its results, so a team of lanes owns a row
+// and keeps it in registers, eight columns ("a chunk") a lane and CH chunks: one wave where n <= 512
+// (four rows a block), else a block of as many waves as the row needs.  The stream h is rounded once,
+// to the activations' type, and the norm is that of the rounded h, whether h is written or not: then
+// the backward pass, which reads h, is the adjoint of what the forward computed.
+// Rows are addressed through a descriptor each, so that columns behind the last and operands that are
+// not there read as zeros and stores to them are dropped: every memory operation is unconditional, and
+// the compiler counts exactly how many are in flight.
 // Included by resbm_matrix.hip.
 #pragma once
 
@@ -17,6 +21,7 @@
 #include <stdint.h>
 
 #include "resbm.h"
+#include "resbm_buffer.hpp"
 #include "resbm_host.hpp"
 
 #ifndef RESBM_IO_F32_BUILD
@@ -25,28 +30,37 @@
 
 namespace resbm_nm {
 
+using resbm::bld16;
+using resbm::bld8;
+using resbm::bst16;
+using resbm::bst8;
+using resbm::make_rsrc;
+using resbm::rsrc_t;
+
 // ---------------------------------------------------------------- eight activations
 #if RESBM_IO_F32_BUILD
 typedef float act_t;
 struct Act8 {
-  float4 a, b;
+  uint4 a, b;
 };
-__device__ __forceinline__ Act8 load8(const act_t* p) { return {((const float4*)p)[0], ((const float4*)p)[1]}; }
-__device__ __forceinline__ void store8(act_t* p, const Act8& v) {
-  ((float4*)p)[0] = v.a;
-  ((float4*)p)[1] = v.b;
+__device__ __forceinline__ Act8 load8(rsrc_t r, int c) {
+  return {bld16(r, (uint32_t)c * 4), bld16(r, (uint32_t)c * 4 + 16)};
 }
-__device__ __forceinline__ Act8 zero8() { return {make_float4(0, 0, 0, 0), make_float4(0, 0, 0, 0)}; }
+__device__ __forceinline__ void store8(rsrc_t r, int c, const Act8& v) {
+  bst16(r, (uint32_t)c * 4, v.a);
+  bst16(r, (uint32_t)c * 4 + 16, v.b);
+}
+__device__ __forceinline__ Act8 load8_by4(rsrc_t r, int c) { return load8(r, c); }
 __device__ __forceinline__ void widen(const Act8& v, float (&f)[8]) {
-  f[0] = v.a.x, f[1] = v.a.y, f[2] = v.a.z, f[3] = v.a.w;
-  f[4] = v.b.x, f[5] = v.b.y, f[6] = v.b.z, f[7] = v.b.w;
+  const uint32_t u[8] = {v.a.x, v.a.y, v.a.z, v.a.w, v.b.x, v.b.y, v.b.z, v.b.w};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = __builtin_bit_cast(float, u[e]);
 }
 __device__ __forceinline__ Act8 narrow(const float (&f)[8]) {
-  return {make_float4(f[0], f[1], f[2], f[3]), make_float4(f[4], f[5], f[6], f[7])};
-}
-__device__ __forceinline__ void widen4(const act_t* p, float (&f)[4]) {
-  const float4 v = *(const float4*)p;
-  f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
+  uint32_t u[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) u[e] = __builtin_bit_cast(uint32_t, f[e]);
+  return {make_uint4(u[0], u[1], u[2], u[3]), make_uint4(u[4], u[5], u[6], u[7])};
 }
 #else
 typedef __bf16 act_t;
@@ -54,9 +68,13 @@ typedef __bf16 nbf2 __attribute__((ext_vector_type(2)));
 struct Act8 {
   uint4 v;
 };
-__device__ __forceinline__ Act8 load8(const act_t* p) { return {*(const uint4*)p}; }
-__device__ __forceinline__ void store8(act_t* p, const Act8& v) { *(uint4*)p = v.v; }
-__device__ __forceinline__ Act8 zero8() { return {make_uint4(0, 0, 0, 0)}; }
+__device__ __forceinline__ Act8 load8(rsrc_t r, int c) { return {bld16(r, (uint32_t)c * 2)}; }
+__device__ __forceinline__ void store8(rsrc_t r, int c, const Act8& v) { bst16(r, (uint32_t)c * 2, v.v); }
+// In two halves: the range of a row of r = 4 mod 8 ends inside a chunk.
+__device__ __forceinline__ Act8 load8_by4(rsrc_t r, int c) {
+  const uint2 a = bld8(r, (uint32_t)c * 2), b = bld8(r, (uint32_t)c * 2 + 8);
+  return {make_uint4(a.x, a.y, b.x, b.y)};
+}
 __device__ __forceinline__ float lo16(uint32_t u) { return __builtin_bit_cast(float, u << 16); }
 __device__ __forceinline__ float hi16(uint32_t u) { return __builtin_bit_cast(float, u & 0xFFFF0000u); }
 __device__ __forceinline__ void widen(const Act8& v, float (&f)[8]) {
@@ -70,17 +88,39 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {  // round to neare
 __device__ __forceinline__ Act8 narrow(const float (&f)[8]) {
   return {make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]))};
 }
-__device__ __forceinline__ void widen4(const act_t* p, float (&f)[4]) {
-  const uint2 v = *(const uint2*)p;
-  f[0] = lo16(v.x), f[1] = hi16(v.x), f[2] = lo16(v.y), f[3] = hi16(v.y);
-}
 #endif
 constexpr size_t kActBytes = sizeof(act_t);
 
-__device__ __forceinline__ void load_gain(const float* gamma, int c, float (&f)[8]) {
-  const float4 a = ((const float4*)(gamma + c))[0], b = ((const float4*)(gamma + c))[1];
-  f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+// Row t of a matrix as a descriptor over its n columns; no columns where p is NULL.
+__device__ __forceinline__ rsrc_t row_of(const act_t* p, int64_t t, int64_t ld, int n) {
+  return make_rsrc(p + t * ld, p ? (int64_t)n * (int64_t)kActBytes : 0);
 }
+__device__ __forceinline__ void load_gain(rsrc_t r, int c, float (&f)[8]) {
+  const uint4 a = bld16(r, (uint32_t)c * 4), b = bld16(r, (uint32_t)c * 4 + 16);
+  const uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = __builtin_bit_cast(float, u[e]);
+}
+
+// The gain of a lane's chunks: kept in registers up to two chunks, read again at each use beyond
+// (from L2; kept, they spilled).
+template <int CH>
+struct Gain {
+  float w[CH <= 2 ? CH : 1][8];
+  __device__ __forceinline__ void keep(rsrc_t r, int lanes, int lane) {
+    if constexpr (CH <= 2)
+#pragma unroll
+      for (int k = 0; k < CH; ++k) load_gain(r, (k * lanes + lane) * 8, w[k]);
+  }
+  __device__ __forceinline__ void get(rsrc_t r, int k, int lanes, int lane, float (&f)[8]) const {
+    if constexpr (CH <= 2) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = w[k][e];
+    } else {
+      load_gain(r, (k * lanes + lane) * 8, f);
+    }
+  }
+};
 
 // ---------------------------------------------------------------- sums and maxima over lanes
 // Lane permutations within 16 lanes (DPP): after steps 1, 2, 4 and 8 every lane holds the result
@@ -120,35 +160,33 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
   return umax(umax(a, b), umax(c, d));
 }
 
-// The team's sum or maximum.  One barrier: the slot alternates, and a slot is written again only
-// behind the barrier of the call in between, which every reader of its old values has passed.
-template <int TEAM>
+// The team's sum or maximum: the wave's own (WAVE), or the block's.  One barrier: the slot alternates,
+// and a slot is written again only behind the barrier of the call in between, which every reader of
+// its old values has passed.  Every 16 lanes add the waves' values in the same order.
+constexpr int kMaxWaves = 16;
+template <bool WAVE>
 struct Team {
-  float* lds;  // 2 * TEAM / 64 words (unused with TEAM == 64)
-  int slot;
-  __device__ __forceinline__ float sum(float v) {
-    v = wave_sum(v);
-    if constexpr (TEAM == 64) return v;
-    float* s = lds + slot * (TEAM / 64);
+  uint32_t* lds;  // 2 * kMaxWaves words
+  int waves, slot;
+  __device__ __forceinline__ uint32_t others(uint32_t v) {
+    uint32_t* s = lds + slot * kMaxWaves;
     slot ^= 1;
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
     __syncthreads();
-    float r = s[0];
-#pragma unroll
-    for (int i = 1; i < TEAM / 64; ++i) r += s[i];
-    return r;
+    const int i = threadIdx.x & 15;
+    return i < waves ? s[i] : 0;
+  }
+  __device__ __forceinline__ float sum(float v) {
+    v = wave_sum(v);
+    if constexpr (WAVE) return v;
+    v = __builtin_bit_cast(float, others(__builtin_bit_cast(uint32_t, v)));
+    return add_step<kMirror>(add_step<kHalfMirror>(add_step<kXor2>(add_step<kXor1>(v))));
   }
   __device__ __forceinline__ uint32_t max(uint32_t v) {
     v = wave_max(v);
-    if constexpr (TEAM == 64) return v;
-    uint32_t* s = (uint32_t*)lds + slot * (TEAM / 64);
-    slot ^= 1;
-    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
-    __syncthreads();
-    uint32_t r = s[0];
-#pragma unroll
-    for (int i = 1; i < TEAM / 64; ++i) r = umax(r, s[i]);
-    return r;
+    if constexpr (WAVE) return v;
+    v = others(v);
+    return max_step<kMirror>(max_step<kHalfMirror>(max_step<kXor2>(max_step<kXor1>(v))));
   }
 };
 
@@ -181,53 +219,54 @@ struct FwdArgs {
   float *scale, *rstd;
 };
 
-template <int TEAM>
-constexpr int block_of() {
-  return TEAM > 256 ? TEAM : 256;
+constexpr int kWaveRows = 4;  // rows of a block whose waves own one each
+template <bool WAVE>
+constexpr int threads_of() {
+  return WAVE ? 64 * kWaveRows : 64 * kMaxWaves;
+}
+template <bool WAVE>
+__device__ __forceinline__ int64_t first_row() {
+  return WAVE ? (int64_t)blockIdx.x * kWaveRows + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : (int64_t)blockIdx.x;
+}
+template <bool WAVE>
+__device__ __forceinline__ int64_t row_step() {
+  return (int64_t)gridDim.x * (WAVE ? kWaveRows : 1);
 }
 
-template <int TEAM, int CH, bool Q8>
-__global__ __launch_bounds__(block_of<TEAM>()) void k_norm_fwd(FwdArgs g) {
-  constexpr int RPB = block_of<TEAM>() / TEAM;  // rows a block has at a time
-  __shared__ float s_red[2 * (TEAM / 64)];
-  Team<TEAM> team{s_red, 0};
-  const int lane = threadIdx.x % TEAM;
-  const int64_t step = (int64_t)gridDim.x * RPB;
-  // a row's wave (TEAM == 64) or block goes through the loop as one: the barriers are uniform
-  for (int64_t t = (int64_t)blockIdx.x * RPB + threadIdx.x / TEAM; t < g.T; t += step) {
-    Act8 h[CH];
+template <bool WAVE, int CH, bool Q8>
+__global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_fwd(FwdArgs g) {
+  __shared__ uint32_t s_red[2 * kMaxWaves];
+  Team<WAVE> team{s_red, (int)blockDim.x >> 6, 0};
+  const int lanes = WAVE ? 64 : (int)blockDim.x, lane = WAVE ? (int)threadIdx.x & 63 : (int)threadIdx.x;
+  const rsrc_t gain = make_rsrc(g.gamma, (int64_t)g.n * 4);
+  // a row's wave or block goes through the loop as one: the barriers are uniform
+  for (int64_t t = first_row<WAVE>(); t < g.T; t += row_step<WAVE>()) {
+    const rsrc_t rx = row_of(g.x, t, g.ld_x, g.n), rr = row_of(g.res, t, g.ld_res, g.n);
+    const rsrc_t rb = row_of(g.b, t, g.r, g.r), rh = row_of(g.h, t, g.ld_h, g.n);
+    Act8 h[CH], a[CH], b[CH];
+    Gain<CH> w;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int c = (k * TEAM + lane) * 8;
-      h[k] = c < g.n ? load8(g.x + t * g.ld_x + c) : zero8();
+      const int c = (k * lanes + lane) * 8;
+      h[k] = load8(rx, c);
+      a[k] = load8(rr, c);
+      b[k] = load8_by4(rb, c);
     }
+    w.keep(gain, lanes, lane);
     float ss = 0.0f;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int c = (k * TEAM + lane) * 8;
-      if (c < g.n) {
-        float f[8];
-        widen(h[k], f);
-        if (g.res) {
-          float v[8];
-          widen(load8(g.res + t * g.ld_res + c), v);
+      float f[8], u[8], v[8];
+      widen(h[k], f);
+      widen(a[k], u);
+      widen(b[k], v);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] += v[e];
-        }
+      for (int e = 0; e < 8; ++e) f[e] = f[e] + u[e] + v[e];
+      h[k] = narrow(f);
+      store8(rh, (k * lanes + lane) * 8, h[k]);
+      widen(h[k], f);
 #pragma unroll
-        for (int q = 0; q < 2; ++q)  // r is a multiple of 4
-          if (c + 4 * q < g.r) {
-            float v[4];
-            widen4(g.b + t * g.r + c + 4 * q, v);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) f[4 * q + e] += v[e];
-          }
-        h[k] = narrow(f);
-        if (g.h) store8(g.h + t * g.ld_h + c, h[k]);
-        widen(h[k], f);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ss += f[e] * f[e];
-      }
+      for (int e = 0; e < 8; ++e) ss += f[e] * f[e];
     }
     const float rstd = 1.0f / sqrtf(team.sum(ss) / (float)g.n + g.eps);
     if (g.rstd && lane == 0) g.rstd[t] = rstd;
@@ -236,14 +275,11 @@ __global__ __launch_bounds__(block_of<TEAM>()) void k_norm_fwd(FwdArgs g) {
       if (g.group == g.n) {
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-          const int c = (k * TEAM + lane) * 8;
-          if (c < g.n) {
-            float f[8], w[8];
-            widen(h[k], f);
-            load_gain(g.gamma, c, w);
+          float f[8], q[8];
+          widen(h[k], f);
+          w.get(gain, k, lanes, lane, q);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) row_max = umax(row_max, mag(f[e] * rstd * w[e]));
-          }
+          for (int e = 0; e < 8; ++e) row_max = umax(row_max, mag(f[e] * rstd * q[e]));
         }
         row_max = team.max(row_max);
         if (lane == 0) g.scale[t] = e4m3_scale(row_max);
@@ -251,38 +287,31 @@ __global__ __launch_bounds__(block_of<TEAM>()) void k_norm_fwd(FwdArgs g) {
     }
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int c = (k * TEAM + lane) * 8;
-      const bool in = c < g.n;
-      float f[8], w[8];
-      if (in) {
-        widen(h[k], f);
-        load_gain(g.gamma, c, w);
+      const int c = (k * lanes + lane) * 8;
+      float f[8], q[8];
+      widen(h[k], f);
+      w.get(gain, k, lanes, lane, q);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = f[e] * rstd * w[e];
-      }
+      for (int e = 0; e < 8; ++e) f[e] = f[e] * rstd * q[e];
       if constexpr (Q8) {
         uint32_t m = row_max;
         if (g.group != g.n) {
-          // groups of 32, 64, 128 or 256 columns: 4, 8, 16 or 32 aligned lanes; a lane without columns gives 0
+          // groups of 32, 64, 128 or 256 columns: 4, 8, 16 or 32 aligned lanes, all of them in the row or none
           m = 0;
-          if (in)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) m = umax(m, mag(f[e]));
+          for (int e = 0; e < 8; ++e) m = umax(m, mag(f[e]));
           m = max_step<kXor2>(max_step<kXor1>(m));
           if (g.group >= 64) m = max_step<kHalfMirror>(m);
           if (g.group >= 128) m = max_step<kMirror>(m);
           if (g.group >= 256) m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
         }
-        if (in) {
-          const float s = e4m3_scale(m), inv = 1.0f / s;
-          if (g.group != g.n && c % g.group == 0) g.scale[t * (g.n / g.group) + c / g.group] = s;
-          uint2 q;
-          q.x = to_e4m3(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
-          q.y = to_e4m3(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv);
-          *(uint2*)((uint8_t*)g.y + t * g.ld_y + c) = q;
-        }
+        const float s = e4m3_scale(m), inv = 1.0f / s;
+        if (g.group != g.n && c < g.n && c % g.group == 0) g.scale[t * (g.n / g.group) + c / g.group] = s;
+        const uint2 code = {to_e4m3(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv),
+                            to_e4m3(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv)};
+        bst8(make_rsrc((uint8_t*)g.y + t * g.ld_y, g.n), (uint32_t)c, code);
       } else {
-        if (in) store8((act_t*)g.y + t * g.ld_y + c, narrow(f));
+        store8(row_of((const act_t*)g.y, t, g.ld_y, g.n), c, narrow(f));
       }
     }
   }
@@ -297,83 +326,142 @@ struct BwdArgs {
   const float *gamma, *rstd;
   act_t* g_x;
   int64_t ld_gx;
+  float* part;    // partial sums of dgamma, [blocks][n], or NULL
+  float* dgamma;  // where one block has all rows
+  int accumulate;
 };
 
-// g_x, a row at a time.
-template <int TEAM, int CH>
-__global__ __launch_bounds__(block_of<TEAM>()) void k_norm_bwd(BwdArgs g) {
-  constexpr int RPB = block_of<TEAM>() / TEAM;
-  __shared__ float s_red[2 * (TEAM / 64)];
-  Team<TEAM> team{s_red, 0};
-  const int lane = threadIdx.x % TEAM;
-  const int64_t step = (int64_t)gridDim.x * RPB;
-  for (int64_t t = (int64_t)blockIdx.x * RPB + threadIdx.x / TEAM; t < g.T; t += step) {
-    Act8 h[CH], gy[CH];
+template <int CH>
+struct BwdRow {
+  Act8 h[CH], gy[CH], gh[CH];
+  float rstd;
+};
+template <int CH>
+__device__ __forceinline__ void load_row(const BwdArgs& g, int64_t t, int lanes, int lane, BwdRow<CH>& v) {
+  const int n = t < g.T ? g.n : 0;  // a row behind the last has no columns
+  t = t < g.T ? t : g.T - 1;
+  const rsrc_t rh = row_of(g.h, t, g.ld_h, n), ry = row_of(g.g_y, t, g.ld_gy, n), rg = row_of(g.g_h, t, g.ld_gh, n);
 #pragma unroll
-    for (int k = 0; k < CH; ++k) {
-      const int c = (k * TEAM + lane) * 8;
-      h[k] = c < g.n ? load8(g.h + t * g.ld_h + c) : zero8();
-      gy[k] = c < g.n ? load8(g.g_y + t * g.ld_gy + c) : zero8();
-    }
-    const float rstd = g.rstd[t];
+  for (int k = 0; k < CH; ++k) {
+    const int c = (k * lanes + lane) * 8;
+    v.h[k] = load8(rh, c);
+    v.gy[k] = load8(ry, c);
+    v.gh[k] = load8(rg, c);
+  }
+  v.rstd = g.rstd[t];
+}
+
+// g_x and (GAIN) dgamma in one pass: a team takes every step-th row, with the next row's loads in
+// flight, and adds its rows' dgamma in registers; a block writes one row of partial sums at the end,
+// its waves' (WAVE) added in wave order.  Without GAIN (rows too wide for that) k_norm_gain forms them.
+template <bool WAVE, int CH, bool GAIN>
+__global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_bwd(BwdArgs g) {
+  __shared__ uint32_t s_red[2 * kMaxWaves];
+  Team<WAVE> team{s_red, (int)blockDim.x >> 6, 0};
+  const int lanes = WAVE ? 64 : (int)blockDim.x, lane = WAVE ? (int)threadIdx.x & 63 : (int)threadIdx.x;
+  const rsrc_t gain = make_rsrc(g.gamma, (int64_t)g.n * 4);
+  Gain<CH> w;
+  w.keep(gain, lanes, lane);
+  float acc[GAIN ? CH : 1][8];
+  if constexpr (GAIN)
+#pragma unroll
+    for (int k = 0; k < CH; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[k][e] = 0.0f;
+  const int64_t step = row_step<WAVE>();
+  BwdRow<CH> row;
+  int64_t t = first_row<WAVE>();
+  if constexpr (GAIN) load_row(g, t, lanes, lane, row);
+  for (; t < g.T; t += step) {
+    BwdRow<CH> next;
+    if constexpr (GAIN)
+      load_row(g, t + step, lanes, lane, next);
+    else
+      load_row(g, t, lanes, lane, row);
     float dot = 0.0f;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int c = (k * TEAM + lane) * 8;
-      if (c < g.n) {
-        float f[8], v[8], w[8];
-        widen(h[k], f);
-        widen(gy[k], v);
-        load_gain(g.gamma, c, w);
+      float f[8], v[8], a[8];
+      widen(row.h[k], f);
+      widen(row.gy[k], v);
+      w.get(gain, k, lanes, lane, a);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dot += v[e] * w[e] * (f[e] * rstd);
+      for (int e = 0; e < 8; ++e) {
+        const float q = v[e] * (f[e] * row.rstd);  // g_y xh
+        if constexpr (GAIN) acc[k][e] += q;
+        dot += q * a[e];
       }
     }
     const float mean = team.sum(dot) / (float)g.n;
+    const rsrc_t ro = row_of(g.g_x, t, g.ld_gx, g.n);
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int c = (k * TEAM + lane) * 8;
-      if (c < g.n) {
-        float f[8], v[8], w[8];
-        widen(h[k], f);
-        widen(gy[k], v);
-        load_gain(g.gamma, c, w);
+      float f[8], v[8], u[8], a[8];
+      widen(row.h[k], f);
+      widen(row.gy[k], v);
+      widen(row.gh[k], u);
+      w.get(gain, k, lanes, lane, a);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = (v[e] * w[e] - f[e] * rstd * mean) * rstd;
-        if (g.g_h) {
-          widen(load8(g.g_h + t * g.ld_gh + c), v);
+      for (int e = 0; e < 8; ++e) f[e] = (v[e] * a[e] - f[e] * row.rstd * mean) * row.rstd + u[e];
+      store8(ro, (k * lanes + lane) * 8, narrow(f));
+    }
+    if constexpr (GAIN) row = next;
+  }
+  if constexpr (GAIN) {
+    __shared__ float s_sum[WAVE ? kWaveRows : 1][WAVE ? CH * 512 : 1];
+    if constexpr (WAVE) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] += v[e];
+      for (int k = 0; k < CH; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s_sum[threadIdx.x >> 6][(k * 64 + lane) * 8 + e] = acc[k][e];
+      __syncthreads();
+      for (int c = threadIdx.x; c < g.n; c += 64 * kWaveRows) {
+        const float s = (s_sum[0][c] + s_sum[1][c]) + (s_sum[2][c] + s_sum[3][c]);
+        if (g.part)
+          g.part[(int64_t)blockIdx.x * g.n + c] = s;
+        else
+          g.dgamma[c] = g.accumulate ? g.dgamma[c] + s : s;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < CH; ++k) {
+        const int c = (k * lanes + lane) * 8;
+        if (c < g.n) {
+          float* out = g.part ? g.part + (int64_t)blockIdx.x * g.n + c : g.dgamma + c;
+          if (!g.part && g.accumulate)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[k][e] += out[e];
+          ((float4*)out)[0] = make_float4(acc[k][0], acc[k][1], acc[k][2], acc[k][3]);
+          ((float4*)out)[1] = make_float4(acc[k][4], acc[k][5], acc[k][6], acc[k][7]);
         }
-        store8(g.g_x + t * g.ld_gx + c, narrow(f));
       }
     }
   }
 }
 
-// Partial sums of dgamma: block (strip, group) adds the rows of its token group in 512 columns,
-// wave w the rows t = w mod 4 of it; the four waves' sums meet in LDS in wave order.
-__global__ __launch_bounds__(256) void k_norm_gain(BwdArgs g, int64_t rows, float* part) {
+// Partial sums of dgamma of wide rows: block (strip, group) adds the rows of its token group in 512
+// columns, wave w the rows t = w mod 4 of it; the four waves' sums meet in LDS in wave order.
+__global__ __launch_bounds__(256) void k_norm_gain(BwdArgs g, int64_t rows) {
   __shared__ float s_sum[4][512];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = (blockIdx.x * 64 + lane) * 8;
   const int64_t t0 = blockIdx.y * rows, t1 = t0 + rows < g.T ? t0 + rows : g.T;
   float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (c < g.n)
-    for (int64_t t = t0 + wave; t < t1; t += 4) {
-      float f[8], v[8];
-      widen(load8(g.h + t * g.ld_h + c), f);
-      widen(load8(g.g_y + t * g.ld_gy + c), v);
-      const float rstd = g.rstd[t];
+#pragma unroll 4
+  for (int64_t t = t0 + wave; t < t1; t += 4) {
+    float f[8], v[8];
+    widen(load8(row_of(g.h, t, g.ld_h, g.n), c), f);
+    widen(load8(row_of(g.g_y, t, g.ld_gy, g.n), c), v);
+    const float rstd = g.rstd[t];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += v[e] * (f[e] * rstd);
-    }
+    for (int e = 0; e < 8; ++e) acc[e] += v[e] * (f[e] * rstd);
+  }
 #pragma unroll
   for (int e = 0; e < 8; ++e) s_sum[wave][lane * 8 + e] = acc[e];
   __syncthreads();
   for (int i = threadIdx.x; i < 512; i += 256) {
     const int col = blockIdx.x * 512 + i;
-    if (col < g.n) part[(int64_t)blockIdx.y * g.n + col] = (s_sum[0][i] + s_sum[1][i]) + (s_sum[2][i] + s_sum[3][i]);
+    if (col < g.n) g.part[(int64_t)blockIdx.y * g.n + col] = (s_sum[0][i] + s_sum[1][i]) + (s_sum[2][i] + s_sum[3][i]);
   }
 }
 
@@ -415,57 +503,65 @@ constexpr int64_t kMaxBlocks = 1 << 20;  // a launch's threads stay below 2^32; 
 
 inline bool width_ok(int64_t T, int n) { return T >= 0 && T <= INT32_MAX && n >= 8 && n <= kMaxWidth && n % 8 == 0; }
 
-// Token groups of the dgamma sums: 64 rows each, at most 256.
+inline int64_t blocks_for(int64_t T, int rpb, int64_t most) {
+  const int64_t b = (T + rpb - 1) / rpb;
+  return b < most ? b : most;
+}
+
+constexpr int kWaveWidth = 512;     // columns that a wave holds in one chunk a lane
+constexpr int kGainWidth = 16384;   // the widest row whose dgamma sums stay in a block's registers
+constexpr int kGainBlocks = 512;    // rows of partial sums, at most
+
+// Blocks (GAIN: each writes a row of partial sums) and rows each takes, all nearly as many.
 struct GainPlan {
   int parts;
   int64_t rows;
 };
-inline GainPlan gain_plan(int64_t T) {
-  int64_t p = (T + 63) / 64;
-  p = p > 256 ? 256 : p;
-  const int64_t rows = (T + p - 1) / p;
-  return {(int)((T + rows - 1) / rows), rows};
+inline GainPlan gain_plan(int64_t T, int n) {
+  const int64_t unit = n <= kWaveWidth ? kWaveRows : n <= kGainWidth ? 1 : 64;
+  const int64_t units = (T + unit - 1) / unit, turns = (units + kGainBlocks - 1) / kGainBlocks;
+  return {(int)((units + turns - 1) / turns), turns * unit};
 }
 
-inline int64_t blocks_for(int64_t T, int rpb) {
-  const int64_t b = (T + rpb - 1) / rpb;
-  return b < kMaxBlocks ? b : kMaxBlocks;
-}
-
-template <int TEAM, int CH, bool Q8>
-void launch_fwd(const FwdArgs& g, hipStream_t s) {
-  constexpr int BLK = block_of<TEAM>();
-  hipLaunchKernelGGL((k_norm_fwd<TEAM, CH, Q8>), dim3((uint32_t)blocks_for(g.T, BLK / TEAM)), dim3(BLK), 0, s, g);
-}
 template <bool Q8>
 void run_fwd(const FwdArgs& g, hipStream_t s) {
-  if (g.n <= 512) return launch_fwd<64, 1, Q8>(g, s);
-  if (g.n <= 2048) return launch_fwd<256, 1, Q8>(g, s);
-  if (g.n <= 4096) return launch_fwd<256, 2, Q8>(g, s);
-  if (g.n <= 8192) return launch_fwd<256, 4, Q8>(g, s);
-  if (g.n <= 16384) return launch_fwd<512, 4, Q8>(g, s);
-  if (g.n <= 32768) return launch_fwd<1024, 4, Q8>(g, s);
-  return launch_fwd<1024, 8, Q8>(g, s);
+  if (g.n <= kWaveWidth) {
+    hipLaunchKernelGGL((k_norm_fwd<true, 1, Q8>), dim3((uint32_t)blocks_for(g.T, kWaveRows, kMaxBlocks)),
+                       dim3(64 * kWaveRows), 0, s, g);
+    return;
+  }
+  const dim3 grid((uint32_t)blocks_for(g.T, 1, kMaxBlocks));
+  const int ch = g.n <= 2048 ? 1 : g.n <= 16384 ? 2 : g.n <= 32768 ? 4 : 8;
+  const dim3 blk(64 * ((g.n + 512 * ch - 1) / (512 * ch)));
+  switch (ch) {
+    case 1: hipLaunchKernelGGL((k_norm_fwd<false, 1, Q8>), grid, blk, 0, s, g); break;
+    case 2: hipLaunchKernelGGL((k_norm_fwd<false, 2, Q8>), grid, blk, 0, s, g); break;
+    case 4: hipLaunchKernelGGL((k_norm_fwd<false, 4, Q8>), grid, blk, 0, s, g); break;
+    default: hipLaunchKernelGGL((k_norm_fwd<false, 8, Q8>), grid, blk, 0, s, g); break;
+  }
 }
 
-template <int TEAM, int CH>
-void launch_bwd(const BwdArgs& g, hipStream_t s) {
-  constexpr int BLK = block_of<TEAM>();
-  hipLaunchKernelGGL((k_norm_bwd<TEAM, CH>), dim3((uint32_t)blocks_for(g.T, BLK / TEAM)), dim3(BLK), 0, s, g);
-}
-inline void run_bwd(const BwdArgs& g, float* part, float* dgamma, int accumulate, hipStream_t s) {
-  const GainPlan p = gain_plan(g.T);
-  // before g_x, which may take g_y's place
-  hipLaunchKernelGGL(k_norm_gain, dim3((g.n + 511) / 512, p.parts), dim3(256), 0, s, g, p.rows, part);
-  hipLaunchKernelGGL(k_norm_gain_sum, dim3((g.n + 31) / 32), dim3(256), 0, s, g.n, p.parts, (const float*)part, dgamma,
-                     accumulate);
-  if (g.n <= 512) return launch_bwd<64, 1>(g, s);
-  if (g.n <= 2048) return launch_bwd<256, 1>(g, s);
-  if (g.n <= 4096) return launch_bwd<256, 2>(g, s);
-  if (g.n <= 8192) return launch_bwd<256, 4>(g, s);
-  if (g.n <= 16384) return launch_bwd<512, 4>(g, s);
-  if (g.n <= 32768) return launch_bwd<1024, 4>(g, s);
-  return launch_bwd<1024, 8>(g, s);
+inline void run_bwd(BwdArgs g, float* ws, hipStream_t s) {
+  const GainPlan p = gain_plan(g.T, g.n);
+  g.part = p.parts > 1 || g.n > kGainWidth ? ws : nullptr;
+  const int ch = g.n <= 2048 ? 1 : g.n <= 16384 ? 2 : g.n <= 32768 ? 4 : 8;
+  const dim3 blk(64 * ((g.n + 512 * ch - 1) / (512 * ch)));
+  const dim3 all((uint32_t)blocks_for(g.T, 1, kMaxBlocks));
+  if (g.n > kGainWidth)  // before g_x, which may take g_y's place
+    hipLaunchKernelGGL(k_norm_gain, dim3((g.n + 511) / 512, p.parts), dim3(256), 0, s, g, p.rows);
+  if (g.n <= kWaveWidth)
+    hipLaunchKernelGGL((k_norm_bwd<true, 1, true>), dim3(p.parts), dim3(64 * kWaveRows), 0, s, g);
+  else if (ch == 1)
+    hipLaunchKernelGGL((k_norm_bwd<false, 1, true>), dim3(p.parts), blk, 0, s, g);
+  else if (ch == 2)
+    hipLaunchKernelGGL((k_norm_bwd<false, 2, true>), dim3(p.parts), blk, 0, s, g);
+  else if (ch == 4)
+    hipLaunchKernelGGL((k_norm_bwd<false, 4, false>), all, blk, 0, s, g);
+  else
+    hipLaunchKernelGGL((k_norm_bwd<false, 8, false>), all, blk, 0, s, g);
+  if (g.part)
+    hipLaunchKernelGGL(k_norm_gain_sum, dim3((g.n + 31) / 32), dim3(256), 0, s, g.n, p.parts, (const float*)g.part,
+                       g.dgamma, g.accumulate);
 }
 
 // Checks and arguments shared by the two forward ops; group == 0: 16-bit (or float32) output.
@@ -525,7 +621,7 @@ extern "C" {
 size_t resbm_norm_workspace_bytes(int64_t T, int32_t n) {
   if (!resbm_nm::width_ok(T, n)) return 0;
   if (T == 0) return 256;
-  return ((size_t)resbm_nm::gain_plan(T).parts * n * 4 + 255) & ~(size_t)255;
+  return ((size_t)resbm_nm::gain_plan(T, n).parts * n * 4 + 255) & ~(size_t)255;
 }
 
 int32_t resbm_skip_norm_fwd(int64_t T, int32_t n, int32_t r, const void* x, int64_t ld_x, const void* res,
@@ -576,7 +672,8 @@ int32_t resbm_skip_norm_bwd(int64_t T, int32_t n, const void* h, int64_t ld_h, c
   g.g_h = (const act_t*)g_h, g.ld_gh = ld_gh;
   g.gamma = gamma, g.rstd = rstd;
   g.g_x = (act_t*)g_x, g.ld_gx = ld_gx;
-  run_bwd(g, (float*)ws, dgamma, accumulate, (hipStream_t)stream);
+  g.dgamma = dgamma, g.accumulate = accumulate;
+  run_bwd(g, (float*)ws, (hipStream_t)stream);
   return launch_status();
 }
 
