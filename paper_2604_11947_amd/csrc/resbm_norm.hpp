@@ -43,14 +43,16 @@ typedef float act_t;
 struct Act8 {
   uint4 a, b;
 };
+template <int POL>
 __device__ __forceinline__ Act8 load8(rsrc_t r, int c) {
-  return {bld16(r, (uint32_t)c * 4), bld16(r, (uint32_t)c * 4 + 16)};
+  return {bld16<POL>(r, (uint32_t)c * 4), bld16<POL>(r, (uint32_t)c * 4 + 16)};
 }
+template <int POL>
 __device__ __forceinline__ void store8(rsrc_t r, int c, const Act8& v) {
-  bst16(r, (uint32_t)c * 4, v.a);
-  bst16(r, (uint32_t)c * 4 + 16, v.b);
+  bst16<POL>(r, (uint32_t)c * 4, v.a);
+  bst16<POL>(r, (uint32_t)c * 4 + 16, v.b);
 }
-__device__ __forceinline__ Act8 load8_by4(rsrc_t r, int c) { return load8(r, c); }
+__device__ __forceinline__ Act8 load8_by4(rsrc_t r, int c) { return load8<0>(r, c); }
 __device__ __forceinline__ void widen(const Act8& v, float (&f)[8]) {
   const uint32_t u[8] = {v.a.x, v.a.y, v.a.z, v.a.w, v.b.x, v.b.y, v.b.z, v.b.w};
 #pragma unroll
@@ -68,8 +70,14 @@ typedef __bf16 nbf2 __attribute__((ext_vector_type(2)));
 struct Act8 {
   uint4 v;
 };
-__device__ __forceinline__ Act8 load8(rsrc_t r, int c) { return {bld16(r, (uint32_t)c * 2)}; }
-__device__ __forceinline__ void store8(rsrc_t r, int c, const Act8& v) { bst16(r, (uint32_t)c * 2, v.v); }
+template <int POL>
+__device__ __forceinline__ Act8 load8(rsrc_t r, int c) {
+  return {bld16<POL>(r, (uint32_t)c * 2)};
+}
+template <int POL>
+__device__ __forceinline__ void store8(rsrc_t r, int c, const Act8& v) {
+  bst16<POL>(r, (uint32_t)c * 2, v.v);
+}
 // In two halves: the range of a row of r = 4 mod 8 ends inside a chunk.
 __device__ __forceinline__ Act8 load8_by4(rsrc_t r, int c) {
   const uint2 a = bld8(r, (uint32_t)c * 2), b = bld8(r, (uint32_t)c * 2 + 8);
@@ -233,7 +241,7 @@ __device__ __forceinline__ int64_t row_step() {
   return (int64_t)gridDim.x * (WAVE ? kWaveRows : 1);
 }
 
-template <bool WAVE, int CH, bool Q8>
+template <bool WAVE, int CH, bool Q8, int POL>
 __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_fwd(FwdArgs g) {
   __shared__ uint32_t s_red[2 * kMaxWaves];
   Team<WAVE> team{s_red, (int)blockDim.x >> 6, 0};
@@ -248,8 +256,8 @@ __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_fwd(FwdArgs g) {
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       const int c = (k * lanes + lane) * 8;
-      h[k] = load8(rx, c);
-      a[k] = load8(rr, c);
+      h[k] = load8<POL>(rx, c);
+      a[k] = load8<POL>(rr, c);
       b[k] = load8_by4(rb, c);
     }
     w.keep(gain, lanes, lane);
@@ -263,7 +271,7 @@ __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_fwd(FwdArgs g) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = f[e] + u[e] + v[e];
       h[k] = narrow(f);
-      store8(rh, (k * lanes + lane) * 8, h[k]);
+      store8<POL>(rh, (k * lanes + lane) * 8, h[k]);
       widen(h[k], f);
 #pragma unroll
       for (int e = 0; e < 8; ++e) ss += f[e] * f[e];
@@ -309,9 +317,9 @@ __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_fwd(FwdArgs g) {
         if (g.group != g.n && c < g.n && c % g.group == 0) g.scale[t * (g.n / g.group) + c / g.group] = s;
         const uint2 code = {to_e4m3(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv),
                             to_e4m3(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv)};
-        bst8(make_rsrc((uint8_t*)g.y + t * g.ld_y, g.n), (uint32_t)c, code);
+        bst8<POL>(make_rsrc((uint8_t*)g.y + t * g.ld_y, g.n), (uint32_t)c, code);
       } else {
-        store8(row_of((const act_t*)g.y, t, g.ld_y, g.n), c, narrow(f));
+        store8<POL>(row_of((const act_t*)g.y, t, g.ld_y, g.n), c, narrow(f));
       }
     }
   }
@@ -336,7 +344,7 @@ struct BwdRow {
   Act8 h[CH], gy[CH], gh[CH];
   float rstd;
 };
-template <int CH>
+template <int POL, int CH>
 __device__ __forceinline__ void load_row(const BwdArgs& g, int64_t t, int lanes, int lane, BwdRow<CH>& v) {
   const int n = t < g.T ? g.n : 0;  // a row behind the last has no columns
   t = t < g.T ? t : g.T - 1;
@@ -344,9 +352,9 @@ __device__ __forceinline__ void load_row(const BwdArgs& g, int64_t t, int lanes,
 #pragma unroll
   for (int k = 0; k < CH; ++k) {
     const int c = (k * lanes + lane) * 8;
-    v.h[k] = load8(rh, c);
-    v.gy[k] = load8(ry, c);
-    v.gh[k] = load8(rg, c);
+    v.h[k] = load8<POL>(rh, c);
+    v.gy[k] = load8<POL>(ry, c);
+    v.gh[k] = load8<POL>(rg, c);
   }
   v.rstd = g.rstd[t];
 }
@@ -354,7 +362,7 @@ __device__ __forceinline__ void load_row(const BwdArgs& g, int64_t t, int lanes,
 // g_x and (GAIN) dgamma in one pass: a team takes every step-th row, with the next row's loads in
 // flight, and adds its rows' dgamma in registers; a block writes one row of partial sums at the end,
 // its waves' (WAVE) added in wave order.  Without GAIN (rows too wide for that) k_norm_gain forms them.
-template <bool WAVE, int CH, bool GAIN>
+template <bool WAVE, int CH, bool GAIN, int POL>
 __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_bwd(BwdArgs g) {
   __shared__ uint32_t s_red[2 * kMaxWaves];
   Team<WAVE> team{s_red, (int)blockDim.x >> 6, 0};
@@ -371,13 +379,13 @@ __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_bwd(BwdArgs g) {
   const int64_t step = row_step<WAVE>();
   BwdRow<CH> row;
   int64_t t = first_row<WAVE>();
-  if constexpr (GAIN) load_row(g, t, lanes, lane, row);
+  if constexpr (GAIN) load_row<POL>(g, t, lanes, lane, row);
   for (; t < g.T; t += step) {
     BwdRow<CH> next;
     if constexpr (GAIN)
-      load_row(g, t + step, lanes, lane, next);
+      load_row<POL>(g, t + step, lanes, lane, next);
     else
-      load_row(g, t, lanes, lane, row);
+      load_row<POL>(g, t, lanes, lane, row);
     float dot = 0.0f;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
@@ -403,7 +411,7 @@ __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_bwd(BwdArgs g) {
       w.get(gain, k, lanes, lane, a);
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = (v[e] * a[e] - f[e] * row.rstd * mean) * row.rstd + u[e];
-      store8(ro, (k * lanes + lane) * 8, narrow(f));
+      store8<POL>(ro, (k * lanes + lane) * 8, narrow(f));
     }
     if constexpr (GAIN) row = next;
   }
@@ -441,6 +449,7 @@ __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_bwd(BwdArgs g) {
 
 // Partial sums of dgamma of wide rows: block (strip, group) adds the rows of its token group in 512
 // columns, wave w the rows t = w mod 4 of it; the four waves' sums meet in LDS in wave order.
+template <int POL>
 __global__ __launch_bounds__(256) void k_norm_gain(BwdArgs g, int64_t rows) {
   __shared__ float s_sum[4][512];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -450,8 +459,8 @@ __global__ __launch_bounds__(256) void k_norm_gain(BwdArgs g, int64_t rows) {
 #pragma unroll 4
   for (int64_t t = t0 + wave; t < t1; t += 4) {
     float f[8], v[8];
-    widen(load8(row_of(g.h, t, g.ld_h, g.n), c), f);
-    widen(load8(row_of(g.g_y, t, g.ld_gy, g.n), c), v);
+    widen(load8<POL>(row_of(g.h, t, g.ld_h, g.n), c), f);
+    widen(load8<POL>(row_of(g.g_y, t, g.ld_gy, g.n), c), v);
     const float rstd = g.rstd[t];
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] += v[e] * (f[e] * rstd);
@@ -503,62 +512,85 @@ constexpr int64_t kMaxBlocks = 1 << 20;  // a launch's threads stay below 2^32; 
 
 inline bool width_ok(int64_t T, int n) { return T >= 0 && T <= INT32_MAX && n >= 8 && n <= kMaxWidth && n % 8 == 0; }
 
-inline int64_t blocks_for(int64_t T, int rpb, int64_t most) {
+inline int64_t blocks_for(int64_t T, int rpb) {
   const int64_t b = (T + rpb - 1) / rpb;
-  return b < most ? b : most;
+  return b < kMaxBlocks ? b : kMaxBlocks;
 }
 
 constexpr int kWaveWidth = 512;     // columns that a wave holds in one chunk a lane
 constexpr int kGainWidth = 16384;   // the widest row whose dgamma sums stay in a block's registers
-constexpr int kGainBlocks = 512;    // rows of partial sums, at most
+constexpr int kStream = 2;          // the cache policy "not to be used again soon"
 
-// Blocks (GAIN: each writes a row of partial sums) and rows each takes, all nearly as many.
+// Loads and stores of tensors that the caches would not hold until their next use bypass them: the
+// 256 MB behind the L2s keep what fits.  Forward at n = 4096, passes over three sets of tensors in turn:
+// 67 MB each 11.7 us cached and 14.0 streaming, 134 MB 26.2 and 24.9, 538 MB 94.6 and 90.7.
+inline bool streams_through(size_t bytes) { return bytes > ((size_t)96 << 20); }
+
+// Blocks of the backward pass (GAIN: each writes a row of partial sums) and rows each takes, all nearly
+// as many.  A multiple of the 256 compute units with about 2^20 columns in all, whose loads for two rows
+// keep HBM busy; more blocks than that only add partial sums and contend: at 16384 x 4096, 256 blocks
+// take 88.5 us, 512 98 us, 1024 107 us; at 32768 x 2048, 256 take 113, 512 93 and 1024 105 us.
 struct GainPlan {
   int parts;
   int64_t rows;
 };
 inline GainPlan gain_plan(int64_t T, int n) {
   const int64_t unit = n <= kWaveWidth ? kWaveRows : n <= kGainWidth ? 1 : 64;
-  const int64_t units = (T + unit - 1) / unit, turns = (units + kGainBlocks - 1) / kGainBlocks;
+  const int64_t fill = (4096 + n / 2) / n;
+  const int64_t most = n <= kWaveWidth ? 512 : 256 * (fill < 1 ? 1 : fill > 4 ? 4 : fill);
+  const int64_t units = (T + unit - 1) / unit, turns = (units + most - 1) / most;
   return {(int)((units + turns - 1) / turns), turns * unit};
 }
 
-template <bool Q8>
+// Chunks a lane.  16-bit output: one while eight waves hold the row (16384 x 4096: 90.7 us against 94.7 with
+// two chunks and 93.2 with four), four beyond (16384 x 8192: 182 against 194 with two; 5120: 116 against 118).
+// 8-bit output, with its maxima: two (16384 x 4096: 80.5 against 84 with one or four; 8192: 159 against 169
+// with four).  Few rows leave compute units idle anyway: as many lanes a row as there are chunks, to shorten
+// each one's chain.
+inline int chunks_fwd(int64_t T, int n, bool q8) {
+  if (n > 16384) return n <= 32768 ? 4 : 8;
+  if (T <= 256 && n <= 8192) return 1;
+  if (q8) return 2;
+  return n <= 4096 ? 1 : 4;
+}
+inline int chunks_bwd(int n) { return n <= 4096 ? 1 : n <= 16384 ? 2 : n <= 32768 ? 4 : 8; }
+inline int block_threads(int n, int ch) { return 64 * ((n + 512 * ch - 1) / (512 * ch)); }
+
+template <bool Q8, int POL>
 void run_fwd(const FwdArgs& g, hipStream_t s) {
   if (g.n <= kWaveWidth) {
-    hipLaunchKernelGGL((k_norm_fwd<true, 1, Q8>), dim3((uint32_t)blocks_for(g.T, kWaveRows, kMaxBlocks)),
-                       dim3(64 * kWaveRows), 0, s, g);
+    hipLaunchKernelGGL((k_norm_fwd<true, 1, Q8, POL>), dim3((uint32_t)blocks_for(g.T, kWaveRows)), dim3(64 * kWaveRows), 0,
+                       s, g);
     return;
   }
-  const dim3 grid((uint32_t)blocks_for(g.T, 1, kMaxBlocks));
-  const int ch = g.n <= 2048 ? 1 : g.n <= 16384 ? 2 : g.n <= 32768 ? 4 : 8;
-  const dim3 blk(64 * ((g.n + 512 * ch - 1) / (512 * ch)));
+  const int ch = chunks_fwd(g.T, g.n, Q8);
+  const dim3 grid((uint32_t)blocks_for(g.T, 1)), blk(block_threads(g.n, ch));
   switch (ch) {
-    case 1: hipLaunchKernelGGL((k_norm_fwd<false, 1, Q8>), grid, blk, 0, s, g); break;
-    case 2: hipLaunchKernelGGL((k_norm_fwd<false, 2, Q8>), grid, blk, 0, s, g); break;
-    case 4: hipLaunchKernelGGL((k_norm_fwd<false, 4, Q8>), grid, blk, 0, s, g); break;
-    default: hipLaunchKernelGGL((k_norm_fwd<false, 8, Q8>), grid, blk, 0, s, g); break;
+    case 1: hipLaunchKernelGGL((k_norm_fwd<false, 1, Q8, POL>), grid, blk, 0, s, g); break;
+    case 2: hipLaunchKernelGGL((k_norm_fwd<false, 2, Q8, POL>), grid, blk, 0, s, g); break;
+    case 4: hipLaunchKernelGGL((k_norm_fwd<false, 4, Q8, POL>), grid, blk, 0, s, g); break;
+    default: hipLaunchKernelGGL((k_norm_fwd<false, 8, Q8, POL>), grid, blk, 0, s, g); break;
   }
 }
 
-inline void run_bwd(BwdArgs g, float* ws, hipStream_t s) {
+template <int POL>
+void run_bwd(BwdArgs g, float* ws, hipStream_t s) {
   const GainPlan p = gain_plan(g.T, g.n);
   g.part = p.parts > 1 || g.n > kGainWidth ? ws : nullptr;
-  const int ch = g.n <= 2048 ? 1 : g.n <= 16384 ? 2 : g.n <= 32768 ? 4 : 8;
-  const dim3 blk(64 * ((g.n + 512 * ch - 1) / (512 * ch)));
-  const dim3 all((uint32_t)blocks_for(g.T, 1, kMaxBlocks));
+  const int ch = chunks_bwd(g.n);
+  const dim3 blk(block_threads(g.n, ch)), all((uint32_t)blocks_for(g.T, 1));
   if (g.n > kGainWidth)  // before g_x, which may take g_y's place
-    hipLaunchKernelGGL(k_norm_gain, dim3((g.n + 511) / 512, p.parts), dim3(256), 0, s, g, p.rows);
+    hipLaunchKernelGGL(k_norm_gain<POL>, dim3((g.n + 511) / 512, p.parts), dim3(256), 0, s, g, p.rows);
   if (g.n <= kWaveWidth)
-    hipLaunchKernelGGL((k_norm_bwd<true, 1, true>), dim3(p.parts), dim3(64 * kWaveRows), 0, s, g);
+    hipLaunchKernelGGL((k_norm_bwd<true, 1, true, POL>), dim3(p.parts), dim3(64 * kWaveRows), 0, s, g);
   else if (ch == 1)
-    hipLaunchKernelGGL((k_norm_bwd<false, 1, true>), dim3(p.parts), blk, 0, s, g);
+    hipLaunchKernelGGL((k_norm_bwd<false, 1, true, POL>), dim3(p.parts), blk, 0, s, g);
   else if (ch == 2)
-    hipLaunchKernelGGL((k_norm_bwd<false, 2, true>), dim3(p.parts), blk, 0, s, g);
+    hipLaunchKernelGGL((k_norm_bwd<false, 2, true, POL>), dim3(p.parts), blk, 0, s, g);
   else if (ch == 4)
-    hipLaunchKernelGGL((k_norm_bwd<false, 4, false>), all, blk, 0, s, g);
+    hipLaunchKernelGGL((k_norm_bwd<false, 4, false, POL>), all, blk, 0, s, g);
   else
-    hipLaunchKernelGGL((k_norm_bwd<false, 8, false>), all, blk, 0, s, g);
+    hipLaunchKernelGGL((k_norm_bwd<false, 8, false, POL>), all, blk, 0, s, g);
   if (g.part)
     hipLaunchKernelGGL(k_norm_gain_sum, dim3((g.n + 31) / 32), dim3(256), 0, s, g.n, p.parts, (const float*)g.part,
                        g.dgamma, g.accumulate);
@@ -607,10 +639,12 @@ inline int32_t fwd(int64_t T, int32_t n, int32_t r, int32_t group, const void* x
   g.h = (act_t*)h, g.ld_h = ld_h;
   g.y = y, g.ld_y = ld_y;
   g.scale = scale, g.rstd = rstd;
+  const hipStream_t st = (hipStream_t)stream;
+  const bool once = streams_through((1 + (res != nullptr) + (h != nullptr)) * (size_t)T * n * kActBytes + (size_t)T * n * (q8 ? 1 : kActBytes));
   if (q8)
-    run_fwd<true>(g, (hipStream_t)stream);
+    once ? run_fwd<true, kStream>(g, st) : run_fwd<true, 0>(g, st);
   else
-    run_fwd<false>(g, (hipStream_t)stream);
+    once ? run_fwd<false, kStream>(g, st) : run_fwd<false, 0>(g, st);
   return launch_status();
 }
 
@@ -673,7 +707,10 @@ int32_t resbm_skip_norm_bwd(int64_t T, int32_t n, const void* h, int64_t ld_h, c
   g.gamma = gamma, g.rstd = rstd;
   g.g_x = (act_t*)g_x, g.ld_gx = ld_gx;
   g.dgamma = dgamma, g.accumulate = accumulate;
-  run_bwd(g, (float*)ws, (hipStream_t)stream);
+  if (streams_through((3 + (g_h != nullptr)) * (size_t)T * n * kActBytes))
+    run_bwd<kStream>(g, (float*)ws, (hipStream_t)stream);
+  else
+    run_bwd<0>(g, (float*)ws, (hipStream_t)stream);
   return launch_status();
 }
 
