@@ -5,7 +5,7 @@
 //     p <- p (1 - lr wd) - (lr / c1) m / (sqrt(v) / sqrt(c2) + eps),   ck = 1 - bk^step,
 // element by element on 16 to 30 bytes an element and some 15 operations, so HBM bounds it, and launch
 // latency where the tensors are small.  One launch therefore covers all tensors: a plan in device memory
-// lists them and, for every chunk of kChunk elements, the tensor that it belongs to.  A block takes a chunk
+// lists them and, for every chunk of one to four thousand elements, the tensor that it belongs to.  A block takes a chunk
 // at a time; a lane takes four consecutive elements, 16 bytes of every float32 array.
 // Arithmetic is float32 in the order written above, every operation rounded once (no contraction), so that
 // results do not depend on the form a tensor is listed in.
@@ -41,10 +41,19 @@ using resbm_nm::wave_max;
 
 constexpr int kBlock = 256;            // elements per scale of an 8-bit state: 64 lanes x 4
 constexpr int kThreads = 256;
-constexpr int kTurns = 2;              // a wave's turns per chunk
-constexpr int kChunk = kThreads * 4 * kTurns;
+constexpr int kTurn = kThreads * 4;    // elements that a block takes at once
+// Turns of a chunk.  float32 states: one (a block's 218 M parameters: 1106 us, with two 1167); 8-bit states, half
+// the bytes: two, with both turns' loads in flight (260 M parameters: 627 us, with one 663 and four 641);
+// gradients alone: four.
+constexpr int kTurns32 = 1, kTurns8 = 2, kTurnsGrad = 4;
 constexpr int64_t kMaxBlocks = 1 << 20;
-constexpr int kNormBlocks = 2048;      // partial sums of the norm
+// Blocks, and partial sums, of the norm: 1024 with four loads a lane in flight read 6.4 to 6.6 TB/s; twice the
+// blocks 5.9, or half 5.1, and so do twice or half the loads.
+constexpr int kNormBlocks = 1024;
+// Shared memory that a streaming step asks for and does not touch: five blocks to a compute unit instead of
+// seven.  Five have enough loads in flight; with more the memory system serves them less evenly (218 M
+// parameters 1056 us against 1082, 260 M in 8 bits 628 against 646; four: 1066 and 658).
+constexpr int kFewerBlocks = 32000;
 constexpr uint32_t kMagic = 0x57414452u;
 
 // The plan, in host and device memory alike: Head, Entry[count], uint32 tensor[chunks].
@@ -56,13 +65,13 @@ struct Entry {
   __bf16* copy;
   int64_t numel, first;  // first: the tensor's first chunk
   float wd;
-  int32_t g16, q8, vec;  // vec: every pointer allows 16-byte (bf16: 8, codes: 4) access
+  int32_t g16, q8, vec, turns;  // vec: every pointer allows 16-byte (bf16: 8, codes: 4) access
 };
 struct Head {
   uint32_t magic, grads_only;
-  int64_t count, chunks, bytes;
+  int64_t count, chunks, bytes, traffic;  // traffic: bytes that a step reads and writes
 };
-static_assert(sizeof(Head) == 32 && sizeof(Entry) == 88, "plan layout");
+static_assert(sizeof(Head) == 40 && sizeof(Entry) == 96, "plan layout");
 
 struct Table {
   const Entry* entry;
@@ -135,10 +144,10 @@ __device__ __forceinline__ void store_codes(void* p, int64_t e, int left, bool v
     if (i < left) q[i] = (uint8_t)(v >> (8 * i));
 }
 __device__ __forceinline__ void store_copy(__bf16* p, int64_t e, int left, bool vec, const float (&f)[4]) {
-  typedef __bf16 b4 __attribute__((ext_vector_type(4)));
-  const b4 v = {(__bf16)f[0], (__bf16)f[1], (__bf16)f[2], (__bf16)f[3]};
+  typedef __bf16 c4 __attribute__((ext_vector_type(4)));
+  const c4 v = {(__bf16)f[0], (__bf16)f[1], (__bf16)f[2], (__bf16)f[3]};
   if (vec && left >= 4) {
-    *(b4*)(p + e) = v;
+    *(c4*)(p + e) = v;
     return;
   }
 #pragma unroll
@@ -156,87 +165,203 @@ __device__ __forceinline__ double power(double b, uint64_t n) {
   return r;
 }
 
-__global__ __launch_bounds__(kThreads) void k_adamw(Table tab, int64_t chunks, Hyper hy) {
+// The step's constants, and the arithmetic of one element.
+struct Step {
+  float fb1, fb2, ob1, ob2, eps, rate, rc2, keep, gs;
+  bool scaled;
+};
+__device__ __forceinline__ void step_element(const Step& s, float& p, float g, float& m, float& v, float& u) {
 #pragma clang fp contract(off)
-  float gs = 1.0f;
+  if (s.scaled) g = g * s.gs;
+  m = m * s.fb1 + g * s.ob1;
+  v = v * s.fb2 + g * s.ob2 * g;
+  u = sqrtf(v);
+  p = p * s.keep - m / (u * s.rc2 + s.eps) * s.rate;
+}
+// m and v = u^2 from their codes.
+__device__ __forceinline__ void decode4(uint32_t cm, uint32_t cu, float ms, float us, float (&m)[4], float (&v)[4]) {
+#pragma clang fp contract(off)
+  from_e4m3(cm, m);
+  from_e4m3(cu, v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    m[i] = m[i] * ms;
+    v[i] = v[i] * us;
+    v[i] = v[i] * v[i];
+  }
+}
+// Codes and scales of a wave's 256 elements.
+__device__ __forceinline__ void encode4(const float (&m)[4], const float (&u)[4], uint32_t& cm, uint32_t& cu, float& ms,
+                                        float& us) {
+  uint32_t am = 0, au = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    am = umax(am, mag(m[i]));
+    au = umax(au, mag(u[i]));
+  }
+  ms = e4m3_scale(wave_max(am)), us = e4m3_scale(wave_max(au));
+  const float im = 1.0f / ms, iu = 1.0f / us;
+  float q[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    q[i] = u[i] * iu;
+    q[i] = u[i] > 0.0f && q[i] < 0x1p-9f ? 0x1p-9f : q[i];
+  }
+  cm = to_e4m3(m[0] * im, m[1] * im, m[2] * im, m[3] * im);
+  cu = to_e4m3(q[0], q[1], q[2], q[3]);
+}
+
+// Accesses that bypass the caches (NT), or not.
+template <bool NT, class V>
+__device__ __forceinline__ V get(const V* p) {
+  if constexpr (NT) return __builtin_nontemporal_load(p);
+  return *p;
+}
+template <bool NT, class V>
+__device__ __forceinline__ void put(V v, V* p) {
+  if constexpr (NT)
+    __builtin_nontemporal_store(v, p);
+  else
+    *p = v;
+}
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+
+// A whole chunk whose pointers allow wide accesses: every load of the chunk is issued before the first use.
+template <bool Q8, bool G16, bool NT>
+__device__ __forceinline__ void whole_chunk(const Entry& t, int64_t at, const Step& s) {
+  const int lane = threadIdx.x & 63;
+  constexpr int N = Q8 ? kTurns8 : kTurns32;
+  f4 P[N], G[N], M[N], V[N];
+  u2 H[N];
+  uint32_t cm[N], cu[N];
+  float ms[N], us[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int64_t e = at + k * kTurn + threadIdx.x * 4;
+    P[k] = get<NT>((const f4*)(t.p + e));
+    if constexpr (G16)
+      H[k] = get<NT>((const u2*)((const uint16_t*)t.g + e));
+    else
+      G[k] = get<NT>((const f4*)((const float*)t.g + e));
+    if constexpr (Q8) {
+      cm[k] = get<NT>((const uint32_t*)((const uint8_t*)t.m + e));
+      cu[k] = get<NT>((const uint32_t*)((const uint8_t*)t.v + e));
+      ms[k] = t.m_scale[e / kBlock];
+      us[k] = t.v_scale[e / kBlock];
+    } else {
+      M[k] = get<NT>((const f4*)((const float*)t.m + e));
+      V[k] = get<NT>((const f4*)((const float*)t.v + e));
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int64_t e = at + k * kTurn + threadIdx.x * 4;
+    float m[4], v[4], u[4];
+    if constexpr (Q8) {
+      decode4(cm[k], cu[k], ms[k], us[k], m, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m[i] = M[k][i], v[i] = V[k][i];
+    }
+    if constexpr (G16)
+      G[k] = f4{__builtin_bit_cast(float, H[k][0] << 16), __builtin_bit_cast(float, H[k][0] & 0xFFFF0000u),
+                __builtin_bit_cast(float, H[k][1] << 16), __builtin_bit_cast(float, H[k][1] & 0xFFFF0000u)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float p = P[k][i];
+      step_element(s, p, G[k][i], m[i], v[i], u[i]);
+      P[k][i] = p;
+    }
+    put<NT>(P[k], (f4*)(t.p + e));
+    if (t.copy) put<NT>((b4{(__bf16)P[k][0], (__bf16)P[k][1], (__bf16)P[k][2], (__bf16)P[k][3]}), (b4*)(t.copy + e));
+    if constexpr (Q8) {
+      uint32_t qm, qu;
+      float sm, su;
+      encode4(m, u, qm, qu, sm, su);
+      put<NT>(qm, (uint32_t*)((uint8_t*)t.m + e));
+      put<NT>(qu, (uint32_t*)((uint8_t*)t.v + e));
+      if (lane == 0) {
+        t.m_scale[e / kBlock] = sm;
+        t.v_scale[e / kBlock] = su;
+      }
+    } else {
+      put<NT>((f4{m[0], m[1], m[2], m[3]}), (f4*)((float*)t.m + e));
+      put<NT>((f4{v[0], v[1], v[2], v[3]}), (f4*)((float*)t.v + e));
+    }
+  }
+}
+
+// A tensor's last chunk, or one whose pointers do not: element by element where need be.
+__device__ __forceinline__ void part_chunk(const Entry& t, int64_t at, const Step& s) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const bool vec = t.vec;
+  for (int k = 0; k < t.turns; ++k) {
+    const int64_t w0 = at + k * kTurn + wave * kBlock;  // the wave's 256 elements
+    if (w0 >= t.numel) break;
+    const int64_t e = w0 + lane * 4, rest = t.numel - e;
+    const int left = rest < 0 ? 0 : rest > 4 ? 4 : (int)rest;
+    float p[4], g[4], m[4], v[4], u[4];
+    load_f32(t.p, e, left, vec, p);
+    load_grad(t, e, left, vec, g);
+    if (t.q8) {
+      decode4(load_codes(t.m, e, left, vec), load_codes(t.v, e, left, vec), t.m_scale[w0 / kBlock], t.v_scale[w0 / kBlock], m, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i >= left) m[i] = v[i] = 0.0f;  // beside a scale that is not finite, no element is 0 times that
+    } else {
+      load_f32((const float*)t.m, e, left, vec, m);
+      load_f32((const float*)t.v, e, left, vec, v);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) step_element(s, p[i], g[i], m[i], v[i], u[i]);
+    store_f32(t.p, e, left, vec, p);
+    if (t.copy) store_copy(t.copy, e, left, vec, p);
+    if (t.q8) {
+      uint32_t qm, qu;
+      float sm, su;
+      encode4(m, u, qm, qu, sm, su);
+      store_codes(t.m, e, left, vec, qm);
+      store_codes(t.v, e, left, vec, qu);
+      if (lane == 0) {
+        t.m_scale[w0 / kBlock] = sm;
+        t.v_scale[w0 / kBlock] = su;
+      }
+    } else {
+      store_f32((float*)t.m, e, left, vec, m);
+      store_f32((float*)t.v, e, left, vec, v);
+    }
+  }
+}
+
+template <bool NT>
+__global__ __launch_bounds__(kThreads) void k_adamw(const Entry* __restrict__ entry, const uint32_t* __restrict__ tensor,
+                                                    int64_t chunks, Hyper hy) {
+  Step s = {hy.fb1, hy.fb2, hy.ob1, hy.ob2, hy.eps, hy.rate, hy.rc2, 1.0f, 1.0f, hy.grad_scale != nullptr};
   if (hy.grad_scale) {
-    gs = *hy.grad_scale;
-    if (gs != gs) return;  // no norm, no step: everything stays as it is
+    s.gs = *hy.grad_scale;
+    if (s.gs != s.gs) return;  // no norm, no step: everything stays as it is
   }
   double lr = hy.lr;
-  float rate = hy.rate, rc2 = hy.rc2;
   if (hy.lr_step) {
     lr = hy.lr_step[0];
     const double step = hy.lr_step[1];
     const uint64_t n = step >= 1.0 ? (step < 1e18 ? (uint64_t)step : (uint64_t)1e18) : 1;
-    rate = (float)(lr / (1.0 - power(hy.b1, n)));
-    rc2 = (float)(1.0 / sqrt(1.0 - power(hy.b2, n)));
+    s.rate = (float)(lr / (1.0 - power(hy.b1, n)));
+    s.rc2 = (float)(1.0 / sqrt(1.0 - power(hy.b2, n)));
   }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const Entry t = tab.entry[tab.tensor[c]];
-    const float keep = (float)(1.0 - lr * (double)t.wd);
-    const bool vec = t.vec;
-#pragma unroll
-    for (int k = 0; k < kTurns; ++k) {
-      const int64_t w0 = (c - t.first) * kChunk + (k * (kThreads / 64) + wave) * kBlock;  // the wave's 256 elements
-      if (w0 >= t.numel) break;
-      const int64_t e = w0 + lane * 4, rest = t.numel - e;
-      const int left = rest < 0 ? 0 : rest > 4 ? 4 : (int)rest;
-      float p[4], g[4], m[4], v[4], u[4];
-      load_f32(t.p, e, left, vec, p);
-      load_grad(t, e, left, vec, g);
-      if (t.q8) {
-        const float ms = t.m_scale[w0 / kBlock], us = t.v_scale[w0 / kBlock];
-        from_e4m3(load_codes(t.m, e, left, vec), m);
-        from_e4m3(load_codes(t.v, e, left, vec), v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          m[i] = m[i] * ms;
-          v[i] = v[i] * us;
-          v[i] = v[i] * v[i];
-          if (i >= left) m[i] = v[i] = 0.0f;
-        }
-      } else {
-        load_f32((const float*)t.m, e, left, vec, m);
-        load_f32((const float*)t.v, e, left, vec, v);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (hy.grad_scale) g[i] = g[i] * gs;
-        m[i] = m[i] * hy.fb1 + g[i] * hy.ob1;
-        v[i] = v[i] * hy.fb2 + g[i] * hy.ob2 * g[i];
-        u[i] = sqrtf(v[i]);
-        p[i] = p[i] * keep - m[i] / (u[i] * rc2 + hy.eps) * rate;
-      }
-      store_f32(t.p, e, left, vec, p);
-      if (t.copy) store_copy(t.copy, e, left, vec, p);
-      if (t.q8) {
-        uint32_t am = 0, au = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          am = umax(am, mag(m[i]));
-          au = umax(au, mag(u[i]));
-        }
-        const float ms = e4m3_scale(wave_max(am)), us = e4m3_scale(wave_max(au));
-        const float im = 1.0f / ms, iu = 1.0f / us;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          m[i] = m[i] * im;
-          const float q = u[i] * iu;
-          u[i] = u[i] > 0.0f && q < 0x1p-9f ? 0x1p-9f : q;
-        }
-        store_codes(t.m, e, left, vec, to_e4m3(m[0], m[1], m[2], m[3]));
-        store_codes(t.v, e, left, vec, to_e4m3(u[0], u[1], u[2], u[3]));
-        if (lane == 0) {
-          t.m_scale[w0 / kBlock] = ms;
-          t.v_scale[w0 / kBlock] = us;
-        }
-      } else {
-        store_f32((float*)t.m, e, left, vec, m);
-        store_f32((float*)t.v, e, left, vec, v);
-      }
-    }
+    const Entry t = entry[tensor[c]];
+    const int64_t at = (c - t.first) * t.turns * kTurn;
+    s.keep = (float)(1.0 - lr * (double)t.wd);
+    if (!t.vec || at + t.turns * kTurn > t.numel)
+      part_chunk(t, at, s);
+    else if (t.q8)
+      t.g16 ? whole_chunk<true, true, NT>(t, at, s) : whole_chunk<true, false, NT>(t, at, s);
+    else
+      t.g16 ? whole_chunk<false, true, NT>(t, at, s) : whole_chunk<false, false, NT>(t, at, s);
   }
 }
 
@@ -252,14 +377,42 @@ __device__ __forceinline__ double block_sum(double v, double* lds) {
   return s;
 }
 
-__global__ __launch_bounds__(kThreads) void k_grad_norm(Table tab, int64_t chunks, double* part) {
+template <bool G16, int N>
+__device__ __forceinline__ double whole_squares(const Entry& t, int64_t at, double s) {
+  f4 g[N];
+  u2 h[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int64_t e = at + k * kTurn + threadIdx.x * 4;
+    if constexpr (G16)
+      h[k] = *(const u2*)((const uint16_t*)t.g + e);
+    else
+      g[k] = *(const f4*)((const float*)t.g + e);
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    if constexpr (G16)
+      g[k] = f4{__builtin_bit_cast(float, h[k][0] << 16), __builtin_bit_cast(float, h[k][0] & 0xFFFF0000u),
+                __builtin_bit_cast(float, h[k][1] << 16), __builtin_bit_cast(float, h[k][1] & 0xFFFF0000u)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s = fma((double)g[k][i], (double)g[k][i], s);
+  }
+  return s;
+}
+
+__global__ __launch_bounds__(kThreads) void k_grad_norm(const Entry* __restrict__ entry, const uint32_t* __restrict__ tensor,
+                                                        int64_t chunks, double* __restrict__ part) {
   __shared__ double s_red[kThreads / 64];
   double s = 0.0;
   for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const Entry t = tab.entry[tab.tensor[c]];
-#pragma unroll
-    for (int k = 0; k < kTurns; ++k) {
-      const int64_t e = (c - t.first) * kChunk + (k * kThreads + threadIdx.x) * 4, rest = t.numel - e;
+    const Entry t = entry[tensor[c]];
+    const int64_t at = (c - t.first) * t.turns * kTurn;
+    if (t.vec && t.turns == kTurnsGrad && at + kTurnsGrad * kTurn <= t.numel) {
+      s = t.g16 ? whole_squares<true, kTurnsGrad>(t, at, s) : whole_squares<false, kTurnsGrad>(t, at, s);
+      continue;
+    }
+    for (int k = 0; k < t.turns; ++k) {
+      const int64_t e = at + k * kTurn + threadIdx.x * 4, rest = t.numel - e;
       const int left = rest < 0 ? 0 : rest > 4 ? 4 : (int)rest;
       float g[4];
       load_grad(t, e, left, t.vec, g);
@@ -271,10 +424,18 @@ __global__ __launch_bounds__(kThreads) void k_grad_norm(Table tab, int64_t chunk
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-__global__ __launch_bounds__(kThreads) void k_grad_norm_out(int parts, const double* part, double max_norm, float* out) {
+// The partial sums of up to kNormBlocks blocks, all loads in flight at once.
+__global__ __launch_bounds__(kThreads) void k_grad_norm_out(int parts, const double* __restrict__ part, double max_norm,
+                                                            float* __restrict__ out) {
   __shared__ double s_red[kThreads / 64];
-  double s = 0.0;
-  for (int i = threadIdx.x; i < parts; i += kThreads) s += part[i];
+  double v[kNormBlocks / kThreads], s = 0.0;
+#pragma unroll
+  for (int k = 0; k < kNormBlocks / kThreads; ++k) {
+    const int i = k * kThreads + threadIdx.x;
+    v[k] = i < parts ? part[i] : 0.0;
+  }
+#pragma unroll
+  for (int k = 0; k < kNormBlocks / kThreads; ++k) s += v[k];
   s = block_sum(s, s_red);
   if (threadIdx.x == 0) {
     const double norm = sqrt(s), f = max_norm / (norm + 1e-6);
@@ -288,7 +449,13 @@ using resbm_host::aligned;
 using resbm_host::launch_status;
 using resbm_host::overlap;
 
-inline int64_t chunks_of(int64_t numel) { return (numel + kChunk - 1) / kChunk; }
+inline int turns_of(const resbm_adamw_tensor& a) {
+  return !a.p ? kTurnsGrad : a.state == RESBM_STATE_E4M3 ? kTurns8 : kTurns32;
+}
+inline int64_t chunks_of(const resbm_adamw_tensor& a) {
+  const int64_t k = (int64_t)turns_of(a) * kTurn;
+  return (a.numel + k - 1) / k;
+}
 inline size_t plan_size(int64_t count, int64_t chunks) {
   return (sizeof(Head) + (size_t)count * sizeof(Entry) + (size_t)chunks * 4 + 255) & ~(size_t)255;
 }
@@ -321,7 +488,7 @@ inline int32_t check_list(const resbm_adamw_tensor* t, int64_t count, int64_t* c
     if (!aligned(a.p, 4) || !aligned(a.g, sg) || !aligned(a.m, ss) || !aligned(a.v, ss) || !aligned(a.copy, 2) ||
         (q8 && (!aligned(a.m_scale, 4) || !aligned(a.v_scale, 4))))
       return RESBM_E_ALIGN;
-    *chunks += chunks_of(a.numel);
+    *chunks += chunks_of(a);
   }
   if (*chunks > INT32_MAX) return RESBM_E_SHAPE;
   if (bare != 0 && bare != work) return RESBM_E_NULL;  // all with parameters and states, or none
@@ -400,19 +567,22 @@ int32_t resbm_adamw_plan(const resbm_adamw_tensor* tensors, int64_t count, void*
   Head* h = (Head*)plan;
   Entry* e = (Entry*)((char*)plan + sizeof(Head));
   uint32_t* at = (uint32_t*)(e + count);
-  int64_t c = 0;
+  int64_t c = 0, traffic = 0;
   for (int64_t i = 0; i < count; ++i) {
     const resbm_adamw_tensor& a = tensors[i];
     const bool q8 = a.state == RESBM_STATE_E4M3, g16 = a.g_type == RESBM_TYPE_BF16;
     e[i] = {a.p, a.g, a.m, a.v, a.m_scale, a.v_scale, (__bf16*)a.copy, a.numel, c, a.weight_decay, g16, q8,
             aligned(a.p, 16) && aligned(a.g, g16 ? 8 : 16) && aligned(a.m, q8 ? 4 : 16) && aligned(a.v, q8 ? 4 : 16) &&
-                aligned(a.copy, 8)};
-    for (int64_t k = chunks_of(a.numel); k > 0; --k) at[c++] = (uint32_t)i;
+                aligned(a.copy, 8),
+            turns_of(a)};
+    traffic += a.numel * ((g16 ? 2 : 4) + (!a.p ? 0 : 8 + (q8 ? 4 : 16) + (a.copy ? 2 : 0)));
+    for (int64_t k = chunks_of(a); k > 0; --k) at[c++] = (uint32_t)i;
   }
   h->grads_only = grads_only;
   h->count = count;
   h->chunks = chunks;
   h->bytes = (int64_t)bytes;
+  h->traffic = traffic;
   h->magic = kMagic;
   return RESBM_OK;
 }
@@ -432,8 +602,13 @@ int32_t resbm_adamw_update(const void* plan, const void* plan_dev, double lr, do
   const Hyper hy = {lr, beta1, beta2, (float)beta1, (float)beta2, (float)(1.0 - beta1), (float)(1.0 - beta2), (float)eps,
                     (float)(lr / (1.0 - pow(beta1, n))), (float)(1.0 / sqrt(1.0 - pow(beta2, n))), lr_step, grad_scale};
   const int64_t blocks = h->chunks < kMaxBlocks ? h->chunks : kMaxBlocks;
-  hipLaunchKernelGGL(k_adamw, dim3((uint32_t)blocks), dim3(kThreads), 0, (hipStream_t)stream, table_of(h, plan_dev),
-                     h->chunks, hy);
+  const Table tab = table_of(h, plan_dev);
+  if (resbm_nm::streams_through((size_t)h->traffic))
+    hipLaunchKernelGGL(k_adamw<true>, dim3((uint32_t)blocks), dim3(kThreads), kFewerBlocks, (hipStream_t)stream, tab.entry, tab.tensor,
+                       h->chunks, hy);
+  else
+    hipLaunchKernelGGL(k_adamw<false>, dim3((uint32_t)blocks), dim3(kThreads), 0, (hipStream_t)stream, tab.entry,
+                       tab.tensor, h->chunks, hy);
   return launch_status();
 }
 
@@ -459,7 +634,8 @@ int32_t resbm_grad_norm(const void* plan, const void* plan_dev, double max_norm,
   const Table tab = table_of(h, plan_dev);
   const int parts = norm_blocks(h->chunks);
   if (parts > 0)
-    hipLaunchKernelGGL(k_grad_norm, dim3(parts), dim3(kThreads), 0, (hipStream_t)stream, tab, h->chunks, (double*)ws);
+    hipLaunchKernelGGL(k_grad_norm, dim3(parts), dim3(kThreads), 0, (hipStream_t)stream, tab.entry, tab.tensor,
+                       h->chunks, (double*)ws);
   hipLaunchKernelGGL(k_grad_norm_out, dim3(1), dim3(kThreads), 0, (hipStream_t)stream, parts, (const double*)ws, max_norm,
                      out);
   return launch_status();
