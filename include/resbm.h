@@ -484,7 +484,8 @@ int32_t resbm_skip_norm_bwd(int64_t T, int32_t n, const void* h, int64_t ld_h,
  *           captured step that is replayed with other values.
  *  grad_scale  NULL, or one device float32, read when the kernel runs.  Where
  *           it is NaN the step is left out: nothing is written.
- * 0 <= b1, b2 < 1; 0 <= eps; step >= 1.
+ * 0 <= b1, b2 < 1; 0 <= eps; step >= 1.  (With eps = 0 an element whose v is
+ * zero becomes 0 / 0, NaN.)
  */
 #define RESBM_TYPE_F32   0
 #define RESBM_TYPE_BF16  1

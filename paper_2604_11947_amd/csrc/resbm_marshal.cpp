@@ -13,6 +13,8 @@
 
 #include <stdint.h>
 
+#include <initializer_list>
+
 namespace {
 
 PyObject* g_raw_stream = nullptr;  // torch._C._cuda_getCurrentRawStream
@@ -236,6 +238,16 @@ PyObject* muon_update(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Whether the tensors that are not None lie on the device of the first.
+void one_device(std::initializer_list<PyObject*> all) {
+  int dev = -1;
+  for (PyObject* o : all) {
+    if (o == Py_None) continue;
+    const int d = (int)THPVariable_Unpack(o).get_device();
+    need(dev < 0 || d == dev);
+    dev = d;
+  }
+}
 void* vector(PyObject* o, int64_t size) {
   const at::Tensor& v = tensor(o, F32);
   need(v.dim() == 1 && v.size(0) == size && v.is_contiguous());
@@ -288,6 +300,7 @@ PyObject* skip_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const NormIn v = norm_in(a);
     int64_t ld_y;
     void* y = strided(a[9], v.io, v.T, v.n, &ld_y);
+    one_device({a[2], a[3], a[4], a[5], a[6], a[7], a[9]});
     return call(a[0], (NormFwd*)nullptr, v.T, dim32(v.n), dim32(v.r), v.x, v.ld_x, v.res, v.ld_res, v.b, v.gamma, v.eps,
                 v.h, v.ld_h, y, ld_y, v.rstd, stream_of(THPVariable_Unpack(a[2])));
   });
@@ -304,6 +317,7 @@ PyObject* skip_norm_q8_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     need(sc.dim() == 2 && sc.size(1) >= 1 && v.n % sc.size(1) == 0);
     const int64_t groups = sc.size(1);
     void* scale = packed(a[10], F32, v.T, groups);
+    one_device({a[2], a[3], a[4], a[5], a[6], a[7], a[9], a[10]});
     return call(a[0], (NormQ8*)nullptr, v.T, dim32(v.n), dim32(v.r), dim32(v.n / groups), v.x, v.ld_x, v.res, v.ld_res,
                 v.b, v.gamma, v.eps, v.h, v.ld_h, y, ld_y, scale, v.rstd, stream_of(THPVariable_Unpack(a[2])));
   });
@@ -327,6 +341,7 @@ PyObject* skip_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const void* gh = strided_or_none(a[8], io, T, nn, &ld_gh);
     const int32_t acc = truth(a[9]);
     const Bytes ws = workspace(a[10]);
+    one_device({a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[10]});
     return call(a[0], (NormBwd*)nullptr, T, dim32(nn), hp, ld_h, ga, rs, gy, ld_gy, gh, ld_gh, gx, ld_gx, dg, acc, ws.p,
                 ws.n, stream_of(h));
   });
@@ -362,8 +377,9 @@ PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&] {
     const at::Tensor& table = tensor(a[2], at::kByte);
     const at::Tensor& out = tensor(a[4], F32);
-    need(out.dim() == 1 && out.size(0) == 2 && out.is_contiguous() && out.get_device() == table.get_device());
+    need(out.dim() == 1 && out.size(0) == 2 && out.is_contiguous());
     const Bytes ws = workspace(a[5]);
+    one_device({a[2], a[4], a[5]});
     return call(a[0], (GradNorm*)nullptr, address(a[1]), table.data_ptr(), real(a[3]), out.data_ptr(), ws.p, ws.n,
                 stream_of(table));
   });

@@ -550,7 +550,10 @@ inline GainPlan gain_plan(int64_t T, int n) {
   const int64_t unit = n <= kWaveWidth ? kWaveRows : n <= kGainWidth ? 1 : 64;
   const int64_t fill = (4096 + n / 2) / n;
   const int64_t most = n <= kWaveWidth ? 512 : 256 * (fill < 1 ? 1 : fill > 4 ? 4 : fill);
-  const int64_t units = (T + unit - 1) / unit, turns = (units + most - 1) / most;
+  const int64_t units = (T + unit - 1) / unit;
+  // up to four rows go through one block, which writes dgamma itself (four rows of 4096: 5.1 us, with a second
+  // launch 7.5)
+  const int64_t turns = units <= 4 && n <= kGainWidth ? units : (units + most - 1) / most;
   return {(int)((units + turns - 1) / turns), turns * unit};
 }
 

@@ -131,6 +131,13 @@ def _vector(t: torch.Tensor, size: int, name: str) -> None:
         raise ValueError(f"{name}: expected a contiguous vector of {size} elements, got {tuple(t.shape)}")
 
 
+def _one_gpu(op: str, *tensors) -> None:
+    """All of an op's tensors on the GPU that the first is on."""
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1 or next(iter(devices)).type != "cuda":
+        raise ValueError(f"{op}: expected tensors of one GPU, got {sorted(map(str, devices))}")
+
+
 def _grad_dtype(t: torch.Tensor, i: int) -> None:
     if t.dtype not in (torch.float32, torch.bfloat16):
         raise TypeError(f"g[{i}]: expected torch.float32 or torch.bfloat16, got {t.dtype}")
@@ -556,6 +563,7 @@ class Library:
         T, n, r, ld_x, ld_res, ld_h = self._norm_inputs(x, gamma, res, b, h, rstd)
         _dtype(y, self.io_dtype, "y")
         ld_y = _ld(y, T, n, "y")
+        _one_gpu("skip_norm_fwd", x, gamma, y, res, b, h, rstd)
         st = self.cdll.resbm_skip_norm_fwd(T, n, r, _ptr(x), ld_x, _ptr(res), ld_res, _ptr(b), _ptr(gamma), eps, _ptr(h),
                                            ld_h, _ptr(y), ld_y, _ptr(rstd), _stream(stream, x))
         self._check("resbm_skip_norm_fwd", st)
@@ -575,6 +583,7 @@ class Library:
         if groups < 1 or n % groups:
             raise ValueError(f"scale: expected shape ({T}, n / group), got {tuple(scale.shape)}")
         _packed(scale, T, groups, "scale")
+        _one_gpu("skip_norm_q8_fwd", x, gamma, y, scale, res, b, h, rstd)
         st = self.cdll.resbm_skip_norm_q8_fwd(T, n, r, n // groups, _ptr(x), ld_x, _ptr(res), ld_res, _ptr(b),
                                               _ptr(gamma), eps, _ptr(h), ld_h, _ptr(y), ld_y, _ptr(scale), _ptr(rstd),
                                               _stream(stream, x))
@@ -597,6 +606,7 @@ class Library:
         ld_gh = _ld(g_h, T, n, "g_h") if g_h is not None else 0
         if ws is None:
             ws = self.norm_workspace(T, n, h.device)
+        _one_gpu("skip_norm_bwd", h, gamma, rstd, g_y, g_x, dgamma, g_h, ws)
         st = self.cdll.resbm_skip_norm_bwd(T, n, _ptr(h), ld_h, _ptr(gamma), _ptr(rstd), _ptr(g_y), ld_gy, _ptr(g_h),
                                            ld_gh, _ptr(g_x), ld_gx, _ptr(dgamma), int(bool(accumulate)), _ptr(ws),
                                            ws.numel(), _stream(stream, h))
@@ -647,10 +657,9 @@ class Library:
 
     def _plan(self, entries, count, lists) -> AdamWPlan:
         tensors = [t for row in lists for t in row if t is not None]
-        devices = {t.device for t in tensors}
-        if len(devices) > 1 or any(d.type != "cuda" for d in devices):
-            raise ValueError(f"a plan's tensors are on one GPU, got {sorted(map(str, devices))}")
-        device = devices.pop() if devices else torch.device("cuda", torch.cuda.current_device())
+        if tensors:
+            _one_gpu("plan", *tensors)
+        device = tensors[0].device if tensors else torch.device("cuda", torch.cuda.current_device())
         nbytes = int(self.cdll.resbm_adamw_plan_bytes(entries, count))
         host = (ctypes.c_int64 * (max(nbytes, 256) // 8))()
         self._check("resbm_adamw_plan", self.cdll.resbm_adamw_plan(entries, count, host, nbytes))
@@ -691,6 +700,7 @@ class Library:
             raise ValueError(f"out: expected a tensor on {plan.device}")
         if ws is None:
             ws = self.grad_norm_workspace(plan)
+        _one_gpu("grad_norm", plan.table, out, ws)
         st = self.cdll.resbm_grad_norm(plan.host_ptr, plan.table_ptr, max_norm, _ptr(out), _ptr(ws), ws.numel(),
                                        _stream(stream, plan))
         self._check("resbm_grad_norm", st)

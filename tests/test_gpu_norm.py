@@ -284,3 +284,41 @@ def test_other_stream_and_no_workspace_race():
         torch.cuda.synchronize()
         for a, b in zip(alone, both):
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_no_rows_and_host_tensors():
+    """T = 0 is no work (dgamma stays), and a host tensor among the operands is refused, native path or not."""
+    L = lib()
+    n = 64
+    x, g = torch.zeros(0, n, dtype=torch.bfloat16, device="cuda"), torch.ones(n, device="cuda")
+    dg = torch.full((n,), 3.0, device="cuda")
+    L.skip_norm_fwd(x, g, torch.zeros_like(x), rstd=torch.zeros(0, device="cuda"))
+    L.skip_norm_q8_fwd(x, g, x.to(torch.float8_e4m3fn), torch.zeros(0, 2, device="cuda"))
+    L.skip_norm_bwd(x, g, torch.zeros(0, device="cuda"), x, torch.zeros_like(x), dg)
+    torch.cuda.synchronize()
+    assert bool((dg == 3.0).all())
+    x = torch.ones(4, n, dtype=torch.bfloat16, device="cuda")
+    y = torch.empty_like(x)
+    with pytest.raises(ValueError, match="one GPU"):
+        L.skip_norm_fwd(x, g.cpu(), y)
+    with pytest.raises(ValueError, match="one GPU"):
+        L.skip_norm_fwd(x, g, y, res=x.cpu())
+    with pytest.raises(ValueError, match="one GPU"):
+        L.skip_norm_bwd(x, g, torch.ones(4, device="cuda"), x, y, dg, ws=torch.zeros(1 << 16, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("T", [2, 3, 4, 5])
+def test_backward_of_few_wide_rows_is_one_block_or_many(T):
+    """Around the row count from which dgamma takes a second launch, on a workspace of the smallest size."""
+    L = lib()
+    for n in (2056, 4096, 16384):
+        d = inputs(T, n, 0, L.io_dtype, 30 + T)
+        rs = torch.rsqrt((d["x"].float() ** 2).mean(1) + EPS)
+        H, G, R_, GY = f64(d["x"]), f64(d["gamma"]), f64(rs), f64(d["gy"])
+        old = torch.randn(n, device="cuda")
+        for acc in (False, True):
+            dg, gx = old.clone(), torch.empty_like(d["x"])
+            L.skip_norm_bwd(d["x"], d["gamma"], rs, d["gy"], gx, dg, accumulate=acc, ws=L.norm_workspace(T, n, "cuda"))
+            _, ref = S.norm_bwd(H, G, R_, GY)
+            ref = ref + (f64(old) if acc else 0)
+            within("dgamma", dg, ref, (T + 4) * U * np.sum(np.abs(GY * H * R_[:, None]), axis=0) + 2 * U * np.abs(ref) + 2.0 ** -133)

@@ -243,5 +243,10 @@ def test_binding_refuses_wrong_tensors(lib):
         lib.adamw_plan(p, p, e, e, m_scale=[torch.zeros(1)], v_scale=[torch.zeros(2)])
     with pytest.raises(ValueError, match="both or neither"):
         lib.adamw_plan(p, p, p, p, v_scale=[torch.zeros(2)])
+    sc, big = torch.zeros(4, 1), torch.zeros(1 << 16, dtype=torch.uint8)
+    for call in (lambda: lib.skip_norm_fwd(x, g, y), lambda: lib.skip_norm_q8_fwd(x, g, q, sc),
+                 lambda: lib.skip_norm_bwd(x, g, torch.ones(4), x, y, torch.zeros(64), ws=big)):
+        with pytest.raises(ValueError, match="one GPU"):  # host memory never reaches a kernel
+            call()
     with pytest.raises(ValueError, match="one GPU"):
         lib.adamw_plan(p, [torch.ones(300)], [torch.ones(300)], [torch.ones(300)])
