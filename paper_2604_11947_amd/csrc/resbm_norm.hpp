@@ -7,13 +7,18 @@
 //     g_x = rstd (w - xh c) + g_h,   dgamma = sum_t g_y xh.
 // Every op reads each operand once and writes each result once, so HBM bounds them (about one
 // operation a byte).  A row has to be whole before any of its results, so a team of lanes owns a row
-// and keeps it in registers, eight columns ("a chunk") a lane and CH chunks: one wave where n <= 512
-// (four rows a block), else a block of as many waves as the row needs.  The stream h is rounded once,
-// to the activations' type, and the norm is that of the rounded h, whether h is written or not: then
-// the backward pass, which reads h, is the adjoint of what the forward computed.
-// Rows are addressed through a descriptor each, so that columns behind the last and operands that are
-// not there read as zeros and stores to them are dropped: every memory operation is unconditional, and
-// the compiler counts exactly how many are in flight.
+// and keeps it in registers, eight columns ("a chunk") a lane and CH chunks: 16, 32 or 64 lanes of a
+// wave where n <= 128, 256 or 512 (four such waves a block), else a block of as many waves as the row
+// needs.  Narrow rows that share a wave: 524288 x 128, no residual, 67 us (6.0 TB/s) against 186 us with a
+// wave each.  The stream h is rounded once, to the activations' type, and the norm is that of the rounded
+// h, whether h is written or not: then the backward pass, which reads h, is the adjoint of what the
+// forward computed.
+// A row that a wave or block has alone is addressed through a descriptor, so that columns behind the
+// last and operands that are not there read as zeros and stores to them are dropped: every memory
+// operation is unconditional, and the compiler counts exactly how many are in flight.
+// Measured, with the passes' minimum bytes: 16384 x 4096 with residual and skip 90.8 us forward (5.9 TB/s)
+// and 87.0 us backward (6.2 TB/s), 8-bit output at 32768 x 8192 319 us (5.9 TB/s); the card's own copy runs
+// at 5.2 TB/s, its in-place sum of two tensors at 5.9.
 // Included by resbm_matrix.hip.
 #pragma once
 
@@ -38,21 +43,55 @@ using resbm::make_rsrc;
 using resbm::rsrc_t;
 
 // ---------------------------------------------------------------- eight activations
+typedef uint32_t w2 __attribute__((ext_vector_type(2)));
+typedef uint32_t w4 __attribute__((ext_vector_type(4)));
+template <int POL>
+__device__ __forceinline__ uint4 get16(const uint4* p) {
+  if constexpr (POL != 0) return __builtin_bit_cast(uint4, __builtin_nontemporal_load((const w4*)p));
+  return *p;
+}
+template <int POL>
+__device__ __forceinline__ void put16(uint4 v, uint4* p) {
+  if constexpr (POL != 0)
+    __builtin_nontemporal_store(__builtin_bit_cast(w4, v), (w4*)p);
+  else
+    *p = v;
+}
+template <int POL>
+__device__ __forceinline__ void put16(uint2 v, uint2* p) {
+  if constexpr (POL != 0)
+    __builtin_nontemporal_store(__builtin_bit_cast(w2, v), (w2*)p);
+  else
+    *p = v;
+}
 #if RESBM_IO_F32_BUILD
 typedef float act_t;
 struct Act8 {
   uint4 a, b;
 };
 template <int POL>
-__device__ __forceinline__ Act8 load8(rsrc_t r, int c) {
-  return {bld16<POL>(r, (uint32_t)c * 4), bld16<POL>(r, (uint32_t)c * 4 + 16)};
+__device__ __forceinline__ Act8 load8(rsrc_t r, uint32_t o) {
+  return {bld16<POL>(r, o * 4), bld16<POL>(r, o * 4 + 16)};
 }
 template <int POL>
-__device__ __forceinline__ void store8(rsrc_t r, int c, const Act8& v) {
-  bst16<POL>(r, (uint32_t)c * 4, v.a);
-  bst16<POL>(r, (uint32_t)c * 4 + 16, v.b);
+__device__ __forceinline__ void store8(rsrc_t r, uint32_t o, const Act8& v) {
+  bst16<POL>(r, o * 4, v.a);
+  bst16<POL>(r, o * 4 + 16, v.b);
 }
-__device__ __forceinline__ Act8 load8_by4(rsrc_t r, int c) { return load8<0>(r, c); }
+template <int POL>
+__device__ __forceinline__ Act8 load8_at(const act_t* p) {
+  return {get16<POL>((const uint4*)p), get16<POL>((const uint4*)p + 1)};
+}
+template <int POL>
+__device__ __forceinline__ void store8_at(act_t* p, const Act8& v) {
+  put16<POL>(v.a, (uint4*)p);
+  put16<POL>(v.b, (uint4*)p + 1);
+}
+__device__ __forceinline__ Act8 load4_4(rsrc_t r, uint32_t o) { return load8<0>(r, o); }
+__device__ __forceinline__ Act8 load4_4(const act_t* p, bool lo, bool hi) {
+  const uint4 z = make_uint4(0, 0, 0, 0);
+  return {lo ? ((const uint4*)p)[0] : z, hi ? ((const uint4*)p)[1] : z};
+}
 __device__ __forceinline__ void widen(const Act8& v, float (&f)[8]) {
   const uint32_t u[8] = {v.a.x, v.a.y, v.a.z, v.a.w, v.b.x, v.b.y, v.b.z, v.b.w};
 #pragma unroll
@@ -71,16 +110,29 @@ struct Act8 {
   uint4 v;
 };
 template <int POL>
-__device__ __forceinline__ Act8 load8(rsrc_t r, int c) {
-  return {bld16<POL>(r, (uint32_t)c * 2)};
+__device__ __forceinline__ Act8 load8(rsrc_t r, uint32_t o) {
+  return {bld16<POL>(r, o * 2)};
 }
 template <int POL>
-__device__ __forceinline__ void store8(rsrc_t r, int c, const Act8& v) {
-  bst16<POL>(r, (uint32_t)c * 2, v.v);
+__device__ __forceinline__ void store8(rsrc_t r, uint32_t o, const Act8& v) {
+  bst16<POL>(r, o * 2, v.v);
 }
-// In two halves: the range of a row of r = 4 mod 8 ends inside a chunk.
-__device__ __forceinline__ Act8 load8_by4(rsrc_t r, int c) {
-  const uint2 a = bld8(r, (uint32_t)c * 2), b = bld8(r, (uint32_t)c * 2 + 8);
+template <int POL>
+__device__ __forceinline__ Act8 load8_at(const act_t* p) {
+  return {get16<POL>((const uint4*)p)};
+}
+template <int POL>
+__device__ __forceinline__ void store8_at(act_t* p, const Act8& v) {
+  put16<POL>(v.v, (uint4*)p);
+}
+// In two halves: a row of r = 4 mod 8 ends inside a chunk.
+__device__ __forceinline__ Act8 load4_4(rsrc_t r, uint32_t o) {
+  const uint2 a = bld8(r, o * 2), b = bld8(r, o * 2 + 8);
+  return {make_uint4(a.x, a.y, b.x, b.y)};
+}
+__device__ __forceinline__ Act8 load4_4(const act_t* p, bool lo, bool hi) {
+  const uint2 z = make_uint2(0, 0);
+  const uint2 a = lo ? ((const uint2*)p)[0] : z, b = hi ? ((const uint2*)p)[1] : z;
   return {make_uint4(a.x, a.y, b.x, b.y)};
 }
 __device__ __forceinline__ float lo16(uint32_t u) { return __builtin_bit_cast(float, u << 16); }
@@ -99,16 +151,55 @@ __device__ __forceinline__ Act8 narrow(const float (&f)[8]) {
 #endif
 constexpr size_t kActBytes = sizeof(act_t);
 
-// Row t of a matrix as a descriptor over its n columns; no columns where p is NULL.
-__device__ __forceinline__ rsrc_t row_of(const act_t* p, int64_t t, int64_t ld, int n) {
-  return make_rsrc(p + t * ld, p ? (int64_t)n * (int64_t)kActBytes : 0);
-}
 __device__ __forceinline__ void load_gain(rsrc_t r, int c, float (&f)[8]) {
   const uint4 a = bld16(r, (uint32_t)c * 4), b = bld16(r, (uint32_t)c * 4 + 16);
   const uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
   for (int e = 0; e < 8; ++e) f[e] = __builtin_bit_cast(float, u[e]);
 }
+
+// A lane's row t of a matrix of n columns.  Where a wave or block has one row (ONE), a descriptor over its
+// columns: behind the last one, and where p is NULL, loads give zeros and stores are dropped.  Where a wave has
+// several, the lane's own address, used where there is a column.
+template <bool ONE, class E>
+struct Row {
+  rsrc_t r;
+  E* p;
+  int cols;
+  __device__ __forceinline__ Row(E* base, int64_t t, int64_t T, int64_t ld, int n) {
+    if constexpr (ONE) {
+      r = make_rsrc(base + t * ld, base ? (int64_t)n * (int64_t)sizeof(E) : 0);  // (t < T here)
+    } else {
+      p = base && t < T ? base + t * ld : base;
+      cols = base && t < T ? n : 0;
+    }
+  }
+  template <int POL>
+  __device__ __forceinline__ Act8 load(int c) const {
+    if constexpr (ONE) return load8<POL>(r, (uint32_t)c);
+    Act8 v = {};
+    if (c < cols) v = load8_at<POL>(p + c);
+    return v;
+  }
+  __device__ __forceinline__ Act8 load_by4(int c) const {
+    if constexpr (ONE) return load4_4(r, (uint32_t)c);
+    return load4_4(p + c, c < cols, c + 4 < cols);
+  }
+  template <int POL>
+  __device__ __forceinline__ void store(int c, const Act8& v) const {
+    if constexpr (ONE)
+      store8<POL>(r, (uint32_t)c, v);
+    else if (c < cols)
+      store8_at<POL>(p + c, v);
+  }
+  template <int POL>
+  __device__ __forceinline__ void store_codes(int c, uint2 v) const {
+    if constexpr (ONE)
+      bst8<POL>(r, (uint32_t)c, v);
+    else if (c < cols)
+      put16<POL>(v, (uint2*)(p + c));
+  }
+};
 
 // The gain of a lane's chunks: kept in registers up to two chunks, read again at each use beyond
 // (from L2; kept, they spilled).
@@ -168,11 +259,34 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
   return umax(umax(a, b), umax(c, d));
 }
 
-// The team's sum or maximum: the wave's own (WAVE), or the block's.  One barrier: the slot alternates,
-// and a slot is written again only behind the barrier of the call in between, which every reader of
-// its old values has passed.  Every 16 lanes add the waves' values in the same order.
+// Lanes that own a row: L = 16, 32 or 64 of a wave, 64 / L rows a wave, or (L = 0) the whole block.
 constexpr int kMaxWaves = 16;
-template <bool WAVE>
+constexpr int kRowWaves = 4;  // waves of a block whose waves own rows
+template <int L>
+struct Shape {
+  static constexpr int kRows = L ? 64 / L : 1;                      // a wave's or block's at a time
+  static constexpr int kBlockRows = L ? kRows * kRowWaves : 1;
+  static constexpr int kThreads = L ? 64 * kRowWaves : 64 * kMaxWaves;  // a block's, at most
+  int lanes, lane, sub;  // a row's lanes, this one among them, and its row among the wave's
+  int64_t first, step;   // the wave's first row, and the distance to its next ones
+  __device__ __forceinline__ explicit Shape(int threads) {  // the block's, from the arguments: blockDim would be
+    const int l = threadIdx.x & 63;                           // read from memory again in the loop
+    lanes = L ? L : threads;
+    lane = L ? l % (L ? L : 1) : (int)threadIdx.x;
+    sub = L ? l / (L ? L : 1) : 0;
+    first = L ? (int64_t)blockIdx.x * kBlockRows + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kRows
+              : (int64_t)blockIdx.x;
+    step = (int64_t)gridDim.x * kBlockRows;
+  }
+  __device__ __forceinline__ int col(int k) const { return (k * lanes + lane) * 8; }
+  template <class E>
+  using Of = Row<kRows == 1, E>;
+};
+
+// The team's sum or maximum: of a row's lanes in their wave, or of the block.  One barrier: the slot
+// alternates, and a slot is written again only behind the barrier of the call in between, which every
+// reader of its old values has passed.  Every 16 lanes add the waves' values in the same order.
+template <int L>
 struct Team {
   uint32_t* lds;  // 2 * kMaxWaves words
   int waves, slot;
@@ -185,14 +299,22 @@ struct Team {
     return i < waves ? s[i] : 0;
   }
   __device__ __forceinline__ float sum(float v) {
+    if constexpr (L == 16 || L == 32) {
+      v = add_step<kMirror>(add_step<kHalfMirror>(add_step<kXor2>(add_step<kXor1>(v))));
+      return L == 16 ? v : v + __shfl_xor(v, 16);
+    }
     v = wave_sum(v);
-    if constexpr (WAVE) return v;
+    if constexpr (L == 64) return v;
     v = __builtin_bit_cast(float, others(__builtin_bit_cast(uint32_t, v)));
     return add_step<kMirror>(add_step<kHalfMirror>(add_step<kXor2>(add_step<kXor1>(v))));
   }
   __device__ __forceinline__ uint32_t max(uint32_t v) {
+    if constexpr (L == 16 || L == 32) {
+      v = max_step<kMirror>(max_step<kHalfMirror>(max_step<kXor2>(max_step<kXor1>(v))));
+      return L == 16 ? v : umax(v, (uint32_t)__shfl_xor((int)v, 16));
+    }
     v = wave_max(v);
-    if constexpr (WAVE) return v;
+    if constexpr (L == 64) return v;
     v = others(v);
     return max_step<kMirror>(max_step<kHalfMirror>(max_step<kXor2>(max_step<kXor1>(v))));
   }
@@ -215,6 +337,7 @@ __device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) 
 // ---------------------------------------------------------------- forward
 struct FwdArgs {
   int64_t T;
+  int threads;  // a block's
   int n, r, group;  // group: columns per scale, n for one a row
   float eps;
   const act_t *x, *res, *b;
@@ -227,38 +350,28 @@ struct FwdArgs {
   float *scale, *rstd;
 };
 
-constexpr int kWaveRows = 4;  // rows of a block whose waves own one each
-template <bool WAVE>
-constexpr int threads_of() {
-  return WAVE ? 64 * kWaveRows : 64 * kMaxWaves;
-}
-template <bool WAVE>
-__device__ __forceinline__ int64_t first_row() {
-  return WAVE ? (int64_t)blockIdx.x * kWaveRows + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : (int64_t)blockIdx.x;
-}
-template <bool WAVE>
-__device__ __forceinline__ int64_t row_step() {
-  return (int64_t)gridDim.x * (WAVE ? kWaveRows : 1);
-}
-
-template <bool WAVE, int CH, bool Q8, int POL>
-__global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_fwd(FwdArgs g) {
+template <int L, int CH, bool Q8, int POL>
+__global__ __launch_bounds__(Shape<L>::kThreads) void k_norm_fwd(FwdArgs g) {
   __shared__ uint32_t s_red[2 * kMaxWaves];
-  Team<WAVE> team{s_red, (int)blockDim.x >> 6, 0};
-  const int lanes = WAVE ? 64 : (int)blockDim.x, lane = WAVE ? (int)threadIdx.x & 63 : (int)threadIdx.x;
+  Team<L> team{s_red, g.threads >> 6, 0};
+  const Shape<L> sh(g.threads);
+  using In = typename Shape<L>::template Of<const act_t>;
+  using Out = typename Shape<L>::template Of<act_t>;
+  const int lanes = sh.lanes, lane = sh.lane;
   const rsrc_t gain = make_rsrc(g.gamma, (int64_t)g.n * 4);
-  // a row's wave or block goes through the loop as one: the barriers are uniform
-  for (int64_t t = first_row<WAVE>(); t < g.T; t += row_step<WAVE>()) {
-    const rsrc_t rx = row_of(g.x, t, g.ld_x, g.n), rr = row_of(g.res, t, g.ld_res, g.n);
-    const rsrc_t rb = row_of(g.b, t, g.r, g.r), rh = row_of(g.h, t, g.ld_h, g.n);
+  // a wave or block goes through the loop as one: the barriers are uniform
+  for (int64_t t0 = sh.first; t0 < g.T; t0 += sh.step) {
+    const int64_t t = t0 + sh.sub;
+    const In rx(g.x, t, g.T, g.ld_x, g.n), rr(g.res, t, g.T, g.ld_res, g.n), rb(g.b, t, g.T, g.r, g.r);
+    const Out rh(g.h, t, g.T, g.ld_h, g.n);
     Act8 h[CH], a[CH], b[CH];
     Gain<CH> w;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int c = (k * lanes + lane) * 8;
-      h[k] = load8<POL>(rx, c);
-      a[k] = load8<POL>(rr, c);
-      b[k] = load8_by4(rb, c);
+      const int c = sh.col(k);
+      h[k] = rx.template load<POL>(c);
+      a[k] = rr.template load<POL>(c);
+      b[k] = rb.load_by4(c);
     }
     w.keep(gain, lanes, lane);
     float ss = 0.0f;
@@ -271,13 +384,14 @@ __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_fwd(FwdArgs g) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = f[e] + u[e] + v[e];
       h[k] = narrow(f);
-      store8<POL>(rh, (k * lanes + lane) * 8, h[k]);
+      rh.template store<POL>(sh.col(k), h[k]);
       widen(h[k], f);
 #pragma unroll
       for (int e = 0; e < 8; ++e) ss += f[e] * f[e];
     }
     const float rstd = 1.0f / sqrtf(team.sum(ss) / (float)g.n + g.eps);
-    if (g.rstd && lane == 0) g.rstd[t] = rstd;
+    const bool live = Shape<L>::kRows == 1 || t < g.T, leads = live && lane == 0;
+    if (g.rstd && leads) g.rstd[t] = rstd;
     uint32_t row_max = 0;
     if constexpr (Q8) {
       if (g.group == g.n) {
@@ -290,12 +404,12 @@ __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_fwd(FwdArgs g) {
           for (int e = 0; e < 8; ++e) row_max = umax(row_max, mag(f[e] * rstd * q[e]));
         }
         row_max = team.max(row_max);
-        if (lane == 0) g.scale[t] = e4m3_scale(row_max);
+        if (leads) g.scale[t] = e4m3_scale(row_max);
       }
     }
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int c = (k * lanes + lane) * 8;
+      const int c = sh.col(k);
       float f[8], q[8];
       widen(h[k], f);
       w.get(gain, k, lanes, lane, q);
@@ -314,12 +428,13 @@ __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_fwd(FwdArgs g) {
           if (g.group >= 256) m = umax(m, (uint32_t)__shfl_xor((int)m, 16));
         }
         const float s = e4m3_scale(m), inv = 1.0f / s;
-        if (g.group != g.n && c < g.n && c % g.group == 0) g.scale[t * (g.n / g.group) + c / g.group] = s;
+        if (g.group != g.n && live && c < g.n && c % g.group == 0)
+          g.scale[t * (g.n / g.group) + c / g.group] = s;
         const uint2 code = {to_e4m3(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv),
                             to_e4m3(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv)};
-        bst8<POL>(make_rsrc((uint8_t*)g.y + t * g.ld_y, g.n), (uint32_t)c, code);
+        typename Shape<L>::template Of<uint8_t>((uint8_t*)g.y, t, g.T, g.ld_y, g.n).template store_codes<POL>(c, code);
       } else {
-        store8<POL>(row_of((const act_t*)g.y, t, g.ld_y, g.n), c, narrow(f));
+        Out((act_t*)g.y, t, g.T, g.ld_y, g.n).template store<POL>(c, narrow(f));
       }
     }
   }
@@ -328,7 +443,7 @@ __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_fwd(FwdArgs g) {
 // ---------------------------------------------------------------- backward
 struct BwdArgs {
   int64_t T;
-  int n;
+  int threads, n;  // threads: a block's
   const act_t *h, *g_y, *g_h;
   int64_t ld_h, ld_gy, ld_gh;
   const float *gamma, *rstd;
@@ -344,29 +459,32 @@ struct BwdRow {
   Act8 h[CH], gy[CH], gh[CH];
   float rstd;
 };
-template <int POL, int CH>
-__device__ __forceinline__ void load_row(const BwdArgs& g, int64_t t, int lanes, int lane, BwdRow<CH>& v) {
-  const int n = t < g.T ? g.n : 0;  // a row behind the last has no columns
-  t = t < g.T ? t : g.T - 1;
-  const rsrc_t rh = row_of(g.h, t, g.ld_h, n), ry = row_of(g.g_y, t, g.ld_gy, n), rg = row_of(g.g_h, t, g.ld_gh, n);
+template <int POL, int L, int CH>
+__device__ __forceinline__ void load_row(const BwdArgs& g, int64_t t0, const Shape<L>& sh, BwdRow<CH>& v) {
+  using In = typename Shape<L>::template Of<const act_t>;
+  const int n = t0 < g.T ? g.n : 0;  // rows behind the last have no columns
+  const int64_t t = (t0 < g.T ? t0 : 0) + sh.sub;
+  const In rh(g.h, t, g.T, g.ld_h, n), ry(g.g_y, t, g.T, g.ld_gy, n), rg(g.g_h, t, g.T, g.ld_gh, n);
 #pragma unroll
   for (int k = 0; k < CH; ++k) {
-    const int c = (k * lanes + lane) * 8;
-    v.h[k] = load8<POL>(rh, c);
-    v.gy[k] = load8<POL>(ry, c);
-    v.gh[k] = load8<POL>(rg, c);
+    const int c = sh.col(k);
+    v.h[k] = rh.template load<POL>(c);
+    v.gy[k] = ry.template load<POL>(c);
+    v.gh[k] = rg.template load<POL>(c);
   }
-  v.rstd = g.rstd[t];
+  v.rstd = g.rstd[t < g.T ? t : g.T - 1];
 }
 
 // g_x and (GAIN) dgamma in one pass: a team takes every step-th row, with the next row's loads in
 // flight, and adds its rows' dgamma in registers; a block writes one row of partial sums at the end,
-// its waves' (WAVE) added in wave order.  Without GAIN (rows too wide for that) k_norm_gain forms them.
-template <bool WAVE, int CH, bool GAIN, int POL>
-__global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_bwd(BwdArgs g) {
+// its waves' rows' (L != 0) added in their order.  Without GAIN (rows too wide for that) k_norm_gain forms them.
+template <int L, int CH, bool GAIN, int POL>
+__global__ __launch_bounds__(Shape<L>::kThreads) void k_norm_bwd(BwdArgs g) {
   __shared__ uint32_t s_red[2 * kMaxWaves];
-  Team<WAVE> team{s_red, (int)blockDim.x >> 6, 0};
-  const int lanes = WAVE ? 64 : (int)blockDim.x, lane = WAVE ? (int)threadIdx.x & 63 : (int)threadIdx.x;
+  Team<L> team{s_red, g.threads >> 6, 0};
+  const Shape<L> sh(g.threads);
+  constexpr int R = Shape<L>::kRows;
+  const int lanes = sh.lanes, lane = sh.lane;
   const rsrc_t gain = make_rsrc(g.gamma, (int64_t)g.n * 4);
   Gain<CH> w;
   w.keep(gain, lanes, lane);
@@ -376,16 +494,15 @@ __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_bwd(BwdArgs g) {
     for (int k = 0; k < CH; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[k][e] = 0.0f;
-  const int64_t step = row_step<WAVE>();
   BwdRow<CH> row;
-  int64_t t = first_row<WAVE>();
-  if constexpr (GAIN) load_row<POL>(g, t, lanes, lane, row);
-  for (; t < g.T; t += step) {
+  int64_t t0 = sh.first;
+  if constexpr (GAIN) load_row<POL>(g, t0, sh, row);
+  for (; t0 < g.T; t0 += sh.step) {
     BwdRow<CH> next;
     if constexpr (GAIN)
-      load_row<POL>(g, t + step, lanes, lane, next);
+      load_row<POL>(g, t0 + sh.step, sh, next);
     else
-      load_row<POL>(g, t, lanes, lane, row);
+      load_row<POL>(g, t0, sh, row);
     float dot = 0.0f;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
@@ -401,7 +518,7 @@ __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_bwd(BwdArgs g) {
       }
     }
     const float mean = team.sum(dot) / (float)g.n;
-    const rsrc_t ro = row_of(g.g_x, t, g.ld_gx, g.n);
+    const typename Shape<L>::template Of<act_t> ro(g.g_x, t0 + sh.sub, g.T, g.ld_gx, g.n);
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       float f[8], v[8], u[8], a[8];
@@ -411,20 +528,22 @@ __global__ __launch_bounds__(threads_of<WAVE>()) void k_norm_bwd(BwdArgs g) {
       w.get(gain, k, lanes, lane, a);
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = (v[e] * a[e] - f[e] * row.rstd * mean) * row.rstd + u[e];
-      store8<POL>(ro, (k * lanes + lane) * 8, narrow(f));
+      ro.template store<POL>(sh.col(k), narrow(f));
     }
     if constexpr (GAIN) row = next;
   }
   if constexpr (GAIN) {
-    __shared__ float s_sum[WAVE ? kWaveRows : 1][WAVE ? CH * 512 : 1];
-    if constexpr (WAVE) {
+    if constexpr (L != 0) {
+      constexpr int S = Shape<L>::kBlockRows;  // rows that have sums of their own
+      __shared__ float s_sum[S][L * 8];
+      const int mine = (int)(threadIdx.x >> 6) * R + sh.sub;
 #pragma unroll
-      for (int k = 0; k < CH; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s_sum[threadIdx.x >> 6][(k * 64 + lane) * 8 + e] = acc[k][e];
+      for (int e = 0; e < 8; ++e) s_sum[mine][lane * 8 + e] = acc[0][e];
       __syncthreads();
-      for (int c = threadIdx.x; c < g.n; c += 64 * kWaveRows) {
-        const float s = (s_sum[0][c] + s_sum[1][c]) + (s_sum[2][c] + s_sum[3][c]);
+      for (int c = threadIdx.x; c < g.n; c += Shape<L>::kThreads) {
+        float s = s_sum[0][c];
+#pragma unroll
+        for (int i = 1; i < S; ++i) s += s_sum[i][c];
         if (g.part)
           g.part[(int64_t)blockIdx.x * g.n + c] = s;
         else
@@ -459,8 +578,8 @@ __global__ __launch_bounds__(256) void k_norm_gain(BwdArgs g, int64_t rows) {
 #pragma unroll 4
   for (int64_t t = t0 + wave; t < t1; t += 4) {
     float f[8], v[8];
-    widen(load8<POL>(row_of(g.h, t, g.ld_h, g.n), c), f);
-    widen(load8<POL>(row_of(g.g_y, t, g.ld_gy, g.n), c), v);
+    widen(Row<true, const act_t>(g.h, t, g.T, g.ld_h, g.n).load<POL>(c), f);
+    widen(Row<true, const act_t>(g.g_y, t, g.T, g.ld_gy, g.n).load<POL>(c), v);
     const float rstd = g.rstd[t];
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] += v[e] * (f[e] * rstd);
@@ -538,6 +657,9 @@ constexpr int kStream = 2;          // the cache policy "not to be used again so
 // 67 MB each 11.7 us cached and 14.0 streaming, 134 MB 26.2 and 24.9, 538 MB 94.6 and 90.7.
 inline bool streams_through(size_t bytes) { return bytes > ((size_t)120 << 20); }
 
+// Lanes of a wave that own a row (0: a block does): several narrow rows share a wave.
+inline int row_lanes(int n) { return n > kWaveWidth ? 0 : n <= 128 ? 16 : n <= 256 ? 32 : 64; }
+
 // Blocks of the backward pass (GAIN: each writes a row of partial sums) and rows each takes, all nearly
 // as many.  A multiple of the 256 compute units with about 2^20 columns in all, whose loads for two rows
 // keep HBM busy; more blocks than that only add partial sums and contend: at 16384 x 4096, 256 blocks
@@ -547,9 +669,10 @@ struct GainPlan {
   int64_t rows;
 };
 inline GainPlan gain_plan(int64_t T, int n) {
-  const int64_t unit = n <= kWaveWidth ? kWaveRows : n <= kGainWidth ? 1 : 64;
+  const int lanes = row_lanes(n);
+  const int64_t unit = lanes ? 64 / lanes * kRowWaves : n <= kGainWidth ? 1 : 64;
   const int64_t fill = (4096 + n / 2) / n;
-  const int64_t most = n <= kWaveWidth ? 512 : 256 * (fill < 1 ? 1 : fill > 4 ? 4 : fill);
+  const int64_t most = lanes ? 512 : 256 * (fill < 1 ? 1 : fill > 4 ? 4 : fill);
   const int64_t units = (T + unit - 1) / unit;
   // up to four rows go through one block, which writes dgamma itself (four rows of 4096: 5.1 us, with a second
   // launch 7.5)
@@ -572,40 +695,53 @@ inline int chunks_bwd(int n) { return n <= 4096 ? 1 : n <= 16384 ? 2 : n <= 3276
 inline int block_threads(int n, int ch) { return 64 * ((n + 512 * ch - 1) / (512 * ch)); }
 
 template <bool Q8, int POL>
-void run_fwd(const FwdArgs& g, hipStream_t s) {
-  if (g.n <= kWaveWidth) {
-    hipLaunchKernelGGL((k_norm_fwd<true, 1, Q8, POL>), dim3((uint32_t)blocks_for(g.T, kWaveRows)), dim3(64 * kWaveRows), 0,
-                       s, g);
+void run_fwd(FwdArgs g, hipStream_t s) {
+  if (const int l = row_lanes(g.n)) {
+    const dim3 few((uint32_t)blocks_for(g.T, 64 / l * kRowWaves)), four(64 * kRowWaves);
+    g.threads = 64 * kRowWaves;
+    if (l == 16)
+      hipLaunchKernelGGL((k_norm_fwd<16, 1, Q8, POL>), few, four, 0, s, g);
+    else if (l == 32)
+      hipLaunchKernelGGL((k_norm_fwd<32, 1, Q8, POL>), few, four, 0, s, g);
+    else
+      hipLaunchKernelGGL((k_norm_fwd<64, 1, Q8, POL>), few, four, 0, s, g);
     return;
   }
   const int ch = chunks_fwd(g.T, g.n, Q8);
   const dim3 grid((uint32_t)blocks_for(g.T, 1)), blk(block_threads(g.n, ch));
+  g.threads = (int)blk.x;
   switch (ch) {
-    case 1: hipLaunchKernelGGL((k_norm_fwd<false, 1, Q8, POL>), grid, blk, 0, s, g); break;
-    case 2: hipLaunchKernelGGL((k_norm_fwd<false, 2, Q8, POL>), grid, blk, 0, s, g); break;
-    case 4: hipLaunchKernelGGL((k_norm_fwd<false, 4, Q8, POL>), grid, blk, 0, s, g); break;
-    default: hipLaunchKernelGGL((k_norm_fwd<false, 8, Q8, POL>), grid, blk, 0, s, g); break;
+    case 1: hipLaunchKernelGGL((k_norm_fwd<0, 1, Q8, POL>), grid, blk, 0, s, g); break;
+    case 2: hipLaunchKernelGGL((k_norm_fwd<0, 2, Q8, POL>), grid, blk, 0, s, g); break;
+    case 4: hipLaunchKernelGGL((k_norm_fwd<0, 4, Q8, POL>), grid, blk, 0, s, g); break;
+    default: hipLaunchKernelGGL((k_norm_fwd<0, 8, Q8, POL>), grid, blk, 0, s, g); break;
   }
 }
 
 template <int POL>
 void run_bwd(BwdArgs g, float* ws, hipStream_t s) {
+  const int l = row_lanes(g.n);
   const GainPlan p = gain_plan(g.T, g.n);
   g.part = p.parts > 1 || g.n > kGainWidth ? ws : nullptr;
   const int ch = chunks_bwd(g.n);
-  const dim3 blk(block_threads(g.n, ch)), all((uint32_t)blocks_for(g.T, 1));
+  const dim3 blk(l ? 64 * kRowWaves : block_threads(g.n, ch)), all((uint32_t)blocks_for(g.T, 1));
+  g.threads = (int)blk.x;
   if (g.n > kGainWidth)  // before g_x, which may take g_y's place
     hipLaunchKernelGGL(k_norm_gain<POL>, dim3((g.n + 511) / 512, p.parts), dim3(256), 0, s, g, p.rows);
-  if (g.n <= kWaveWidth)
-    hipLaunchKernelGGL((k_norm_bwd<true, 1, true, POL>), dim3(p.parts), dim3(64 * kWaveRows), 0, s, g);
+  if (l == 16)
+    hipLaunchKernelGGL((k_norm_bwd<16, 1, true, POL>), dim3(p.parts), blk, 0, s, g);
+  else if (l == 32)
+    hipLaunchKernelGGL((k_norm_bwd<32, 1, true, POL>), dim3(p.parts), blk, 0, s, g);
+  else if (l == 64)
+    hipLaunchKernelGGL((k_norm_bwd<64, 1, true, POL>), dim3(p.parts), blk, 0, s, g);
   else if (ch == 1)
-    hipLaunchKernelGGL((k_norm_bwd<false, 1, true, POL>), dim3(p.parts), blk, 0, s, g);
+    hipLaunchKernelGGL((k_norm_bwd<0, 1, true, POL>), dim3(p.parts), blk, 0, s, g);
   else if (ch == 2)
-    hipLaunchKernelGGL((k_norm_bwd<false, 2, true, POL>), dim3(p.parts), blk, 0, s, g);
+    hipLaunchKernelGGL((k_norm_bwd<0, 2, true, POL>), dim3(p.parts), blk, 0, s, g);
   else if (ch == 4)
-    hipLaunchKernelGGL((k_norm_bwd<false, 4, false, POL>), all, blk, 0, s, g);
+    hipLaunchKernelGGL((k_norm_bwd<0, 4, false, POL>), all, blk, 0, s, g);
   else
-    hipLaunchKernelGGL((k_norm_bwd<false, 8, false, POL>), all, blk, 0, s, g);
+    hipLaunchKernelGGL((k_norm_bwd<0, 8, false, POL>), all, blk, 0, s, g);
   if (g.part)
     hipLaunchKernelGGL(k_norm_gain_sum, dim3((g.n + 31) / 32), dim3(512), 0, s, g.n, p.parts, (const float*)g.part,
                        g.dgamma, g.accumulate);
