@@ -71,7 +71,7 @@ struct Head {
   uint32_t magic, grads_only;
   int64_t count, chunks, bytes, traffic;  // traffic: bytes that a step reads and writes
 };
-static_assert(sizeof(Head) == 40 && sizeof(Entry) == 96, "plan layout");
+static_assert(sizeof(Head) == 40 && sizeof(Entry) == 96 && sizeof(resbm_adamw_tensor) == 80, "layouts");
 
 struct Table {
   const Entry* entry;

@@ -615,7 +615,8 @@ class Library:
     # ------------------------------------------------------------ AdamW over many tensors
     def adamw_plan(self, p, g, m, v, m_scale=None, v_scale=None, copy=None, weight_decay=0.0) -> AdamWPlan:
         """The plan of the lists' tensors: float32 ``p``, gradients float32 or bf16, states float32 or, with
-        ``m_scale`` and ``v_scale`` (an entry may be None), float8_e4m3fn; ``copy``: bf16 tensors or None."""
+        ``m_scale`` and ``v_scale`` (an entry may be None), float8_e4m3fn; ``copy``: bf16 tensors or None.
+        It copies its table to the device, so it is made outside a graph capture; its updates may be captured."""
         k = len(p)
         none = [None] * k
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * k

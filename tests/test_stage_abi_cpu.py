@@ -138,6 +138,10 @@ def test_plan_refusals(lib, over, status):
     assert plan_of(lib, entry(**over))[0] == status
 
 
+def test_entry_layout():
+    assert ctypes.sizeof(R.AdamWTensor) == 80 and R.AdamWTensor.weight_decay.offset == 72 and R.AdamWTensor.copy.offset == 56
+
+
 def test_plan_of_many(lib):
     assert plan_of(lib)[0] == R.OK
     assert plan_of(lib, entry(), moved(1))[0] == R.OK
