@@ -269,14 +269,15 @@ struct Shape {
   static constexpr int kThreads = L ? 64 * kRowWaves : 64 * kMaxWaves;  // a block's, at most
   int lanes, lane, sub;  // a row's lanes, this one among them, and its row among the wave's
   int64_t first, step;   // the wave's first row, and the distance to its next ones
-  __device__ __forceinline__ explicit Shape(int threads) {  // the block's, from the arguments: blockDim would be
-    const int l = threadIdx.x & 63;                           // read from memory again in the loop
+  // threads: the block's, from the arguments (blockDim would be read from memory again in the loop);
+  // others: blocks before the first that owns rows
+  __device__ __forceinline__ Shape(int threads, int others) {
+    const int l = threadIdx.x & 63, block = (int)blockIdx.x - others;
     lanes = L ? L : threads;
     lane = L ? l % (L ? L : 1) : (int)threadIdx.x;
     sub = L ? l / (L ? L : 1) : 0;
-    first = L ? (int64_t)blockIdx.x * kBlockRows + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kRows
-              : (int64_t)blockIdx.x;
-    step = (int64_t)gridDim.x * kBlockRows;
+    first = L ? (int64_t)block * kBlockRows + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kRows : (int64_t)block;
+    step = (int64_t)((int)gridDim.x - others) * kBlockRows;
   }
   __device__ __forceinline__ int col(int k) const { return (k * lanes + lane) * 8; }
   template <class E>
@@ -354,7 +355,7 @@ template <int L, int CH, bool Q8, int POL>
 __global__ __launch_bounds__(Shape<L>::kThreads) void k_norm_fwd(FwdArgs g) {
   __shared__ uint32_t s_red[2 * kMaxWaves];
   Team<L> team{s_red, g.threads >> 6, 0};
-  const Shape<L> sh(g.threads);
+  const Shape<L> sh(g.threads, 0);
   using In = typename Shape<L>::template Of<const act_t>;
   using Out = typename Shape<L>::template Of<act_t>;
   const int lanes = sh.lanes, lane = sh.lane;
@@ -449,9 +450,10 @@ struct BwdArgs {
   const float *gamma, *rstd;
   act_t* g_x;
   int64_t ld_gx;
-  float* part;    // partial sums of dgamma, [blocks][n], or NULL
-  float* dgamma;  // where one block has all rows
+  float* part;  // partial sums of dgamma, [blocks][n]
+  float* dgamma;
   int accumulate;
+  int strips;  // blocks that form dgamma of 64 columns each, before those that own rows
 };
 
 template <int CH>
@@ -475,16 +477,57 @@ __device__ __forceinline__ void load_row(const BwdArgs& g, int64_t t0, const Sha
   v.rstd = g.rstd[t < g.T ? t : g.T - 1];
 }
 
+// dgamma of 64 columns over all rows: eight lanes across, the block's others down, which add every
+// (threads / 8)-th row each; their sums meet within a wave, then in wave order.
+__device__ __forceinline__ void gain_strip(const BwdArgs& g, float (&s_sum)[kMaxWaves][64]) {
+  const int q = threadIdx.x & 7, down = g.threads >> 3;
+  const int c = (int)blockIdx.x * 64 + q * 8;
+  float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (c < g.n) {
+#pragma unroll 4
+    for (int64_t t = threadIdx.x >> 3; t < g.T; t += down) {
+      float f[8], v[8];
+      widen(load8_at<0>(g.h + t * g.ld_h + c), f);
+      widen(load8_at<0>(g.g_y + t * g.ld_gy + c), v);
+      const float rstd = g.rstd[t];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += v[e] * (f[e] * rstd);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+#pragma unroll
+    for (int o = 8; o <= 32; o <<= 1) acc[e] += __shfl_xor(acc[e], o);
+    if ((threadIdx.x & 63) < 8) s_sum[threadIdx.x >> 6][q * 8 + e] = acc[e];
+  }
+  __syncthreads();
+  const int col = (int)blockIdx.x * 64 + (int)threadIdx.x;
+  if (threadIdx.x < 64 && col < g.n) {
+    float s = s_sum[0][threadIdx.x];
+    for (int i = 1; i < g.threads >> 6; ++i) s += s_sum[i][threadIdx.x];
+    g.dgamma[col] = g.accumulate ? g.dgamma[col] + s : s;
+  }
+}
+
 // g_x and (GAIN) dgamma in one pass: a team takes every step-th row, with the next row's loads in
 // flight, and adds its rows' dgamma in registers; a block writes one row of partial sums at the end,
-// its waves' rows' (L != 0) added in their order.  Without GAIN (rows too wide for that) k_norm_gain forms them.
+// its waves' rows' (L != 0) added in their order.  Without GAIN: few rows, whose dgamma is formed beside
+// them (gain_strip: it takes rstd and not the rows' means, so neither waits for the other), or rows too
+// wide for sums in registers (k_norm_gain).
 template <int L, int CH, bool GAIN, int POL>
 __global__ __launch_bounds__(Shape<L>::kThreads) void k_norm_bwd(BwdArgs g) {
   __shared__ uint32_t s_red[2 * kMaxWaves];
   Team<L> team{s_red, g.threads >> 6, 0};
-  const Shape<L> sh(g.threads);
+  const Shape<L> sh(g.threads, GAIN ? 0 : g.strips);
   constexpr int R = Shape<L>::kRows;
   const int lanes = sh.lanes, lane = sh.lane;
+  if constexpr (!GAIN) {
+    if ((int)blockIdx.x < g.strips) {
+      __shared__ float s_gain[kMaxWaves][64];
+      gain_strip(g, s_gain);
+      return;
+    }
+  }
   const rsrc_t gain = make_rsrc(g.gamma, (int64_t)g.n * 4);
   Gain<CH> w;
   w.keep(gain, lanes, lane);
@@ -544,20 +587,14 @@ __global__ __launch_bounds__(Shape<L>::kThreads) void k_norm_bwd(BwdArgs g) {
         float s = s_sum[0][c];
 #pragma unroll
         for (int i = 1; i < S; ++i) s += s_sum[i][c];
-        if (g.part)
-          g.part[(int64_t)blockIdx.x * g.n + c] = s;
-        else
-          g.dgamma[c] = g.accumulate ? g.dgamma[c] + s : s;
+        g.part[(int64_t)blockIdx.x * g.n + c] = s;
       }
     } else {
 #pragma unroll
       for (int k = 0; k < CH; ++k) {
         const int c = (k * lanes + lane) * 8;
         if (c < g.n) {
-          float* out = g.part ? g.part + (int64_t)blockIdx.x * g.n + c : g.dgamma + c;
-          if (!g.part && g.accumulate)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) acc[k][e] += out[e];
+          float* out = g.part + (int64_t)blockIdx.x * g.n + c;
           ((float4*)out)[0] = make_float4(acc[k][0], acc[k][1], acc[k][2], acc[k][3]);
           ((float4*)out)[1] = make_float4(acc[k][4], acc[k][5], acc[k][6], acc[k][7]);
         }
@@ -568,7 +605,6 @@ __global__ __launch_bounds__(Shape<L>::kThreads) void k_norm_bwd(BwdArgs g) {
 
 // Partial sums of dgamma of wide rows: block (strip, group) adds the rows of its token group in 512
 // columns, wave w the rows t = w mod 4 of it; the four waves' sums meet in LDS in wave order.
-template <int POL>
 __global__ __launch_bounds__(256) void k_norm_gain(BwdArgs g, int64_t rows) {
   __shared__ float s_sum[4][512];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -578,8 +614,8 @@ __global__ __launch_bounds__(256) void k_norm_gain(BwdArgs g, int64_t rows) {
 #pragma unroll 4
   for (int64_t t = t0 + wave; t < t1; t += 4) {
     float f[8], v[8];
-    widen(Row<true, const act_t>(g.h, t, g.T, g.ld_h, g.n).load<POL>(c), f);
-    widen(Row<true, const act_t>(g.g_y, t, g.T, g.ld_gy, g.n).load<POL>(c), v);
+    widen(Row<true, const act_t>(g.h, t, g.T, g.ld_h, g.n).load<0>(c), f);
+    widen(Row<true, const act_t>(g.g_y, t, g.T, g.ld_gy, g.n).load<0>(c), v);
     const float rstd = g.rstd[t];
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] += v[e] * (f[e] * rstd);
@@ -674,9 +710,7 @@ inline GainPlan gain_plan(int64_t T, int n) {
   const int64_t fill = (4096 + n / 2) / n;
   const int64_t most = lanes ? 512 : 256 * (fill < 1 ? 1 : fill > 4 ? 4 : fill);
   const int64_t units = (T + unit - 1) / unit;
-  // up to four rows go through one block, which writes dgamma itself (four rows of 4096: 5.1 us, with a second
-  // launch 7.5)
-  const int64_t turns = units <= 4 && n <= kGainWidth ? units : (units + most - 1) / most;
+  const int64_t turns = (units + most - 1) / most;
   return {(int)((units + turns - 1) / turns), turns * unit};
 }
 
@@ -718,33 +752,60 @@ void run_fwd(FwdArgs g, hipStream_t s) {
   }
 }
 
-template <int POL>
-void run_bwd(BwdArgs g, float* ws, hipStream_t s) {
-  const int l = row_lanes(g.n);
-  const GainPlan p = gain_plan(g.T, g.n);
-  g.part = p.parts > 1 || g.n > kGainWidth ? ws : nullptr;
-  const int ch = chunks_bwd(g.n);
-  const dim3 blk(l ? 64 * kRowWaves : block_threads(g.n, ch)), all((uint32_t)blocks_for(g.T, 1));
-  g.threads = (int)blk.x;
-  if (g.n > kGainWidth)  // before g_x, which may take g_y's place
-    hipLaunchKernelGGL(k_norm_gain<POL>, dim3((g.n + 511) / 512, p.parts), dim3(256), 0, s, g, p.rows);
+template <bool GAIN, int POL>
+void launch_bwd(const BwdArgs& g, int l, int ch, dim3 grid, hipStream_t s) {
+  const dim3 blk(g.threads);
   if (l == 16)
-    hipLaunchKernelGGL((k_norm_bwd<16, 1, true, POL>), dim3(p.parts), blk, 0, s, g);
+    hipLaunchKernelGGL((k_norm_bwd<16, 1, GAIN, POL>), grid, blk, 0, s, g);
   else if (l == 32)
-    hipLaunchKernelGGL((k_norm_bwd<32, 1, true, POL>), dim3(p.parts), blk, 0, s, g);
+    hipLaunchKernelGGL((k_norm_bwd<32, 1, GAIN, POL>), grid, blk, 0, s, g);
   else if (l == 64)
-    hipLaunchKernelGGL((k_norm_bwd<64, 1, true, POL>), dim3(p.parts), blk, 0, s, g);
+    hipLaunchKernelGGL((k_norm_bwd<64, 1, GAIN, POL>), grid, blk, 0, s, g);
   else if (ch == 1)
-    hipLaunchKernelGGL((k_norm_bwd<0, 1, true, POL>), dim3(p.parts), blk, 0, s, g);
-  else if (ch == 2)
-    hipLaunchKernelGGL((k_norm_bwd<0, 2, true, POL>), dim3(p.parts), blk, 0, s, g);
-  else if (ch == 4)
-    hipLaunchKernelGGL((k_norm_bwd<0, 4, false, POL>), all, blk, 0, s, g);
+    hipLaunchKernelGGL((k_norm_bwd<0, 1, GAIN, POL>), grid, blk, 0, s, g);
   else
-    hipLaunchKernelGGL((k_norm_bwd<0, 8, false, POL>), all, blk, 0, s, g);
-  if (g.part)
-    hipLaunchKernelGGL(k_norm_gain_sum, dim3((g.n + 31) / 32), dim3(512), 0, s, g.n, p.parts, (const float*)g.part,
-                       g.dgamma, g.accumulate);
+    hipLaunchKernelGGL((k_norm_bwd<0, 2, GAIN, POL>), grid, blk, 0, s, g);
+}
+inline void launch_wide(const BwdArgs& g, int ch, dim3 grid, hipStream_t s) {
+  if (ch == 4)
+    hipLaunchKernelGGL((k_norm_bwd<0, 4, false, 0>), grid, dim3(g.threads), 0, s, g);
+  else
+    hipLaunchKernelGGL((k_norm_bwd<0, 8, false, 0>), grid, dim3(g.threads), 0, s, g);
+}
+
+// Whether dgamma is formed beside the rows, in the same launch: up to eight rows a lane (a block's threads / 8
+// rows go down at once), where that takes no longer than the second launch (n = 2048, 128 rows 4.5 us against
+// 7.4, 256 rows 5.8 against 7.4, 512 rows 14 against 7.6; n = 1024, 128 rows 5.4 against 7.1, 256 rows 7.7
+// against 7.1; n = 4096, 256 rows 6.5 against 7.6, 512 rows 10.7 against 8.5).
+inline bool few_rows(int64_t T, int threads) { return T <= 256 && T <= threads; }
+
+inline void run_bwd(BwdArgs g, float* ws, hipStream_t s) {
+  const int l = row_lanes(g.n), ch = chunks_bwd(g.n);
+  const bool wide = g.n > kGainWidth;
+  const dim3 all((uint32_t)blocks_for(g.T, l ? 64 / l * kRowWaves : 1));
+  g.threads = l ? 64 * kRowWaves : block_threads(g.n, ch);
+  if (few_rows(g.T, g.threads)) {
+    // one launch, or two where g_x takes the place of g_y, which dgamma reads
+    const int strips = (g.n + 63) / 64;
+    const bool place = g.g_x == g.g_y;
+    for (int pass = place ? 0 : 1; pass < 2; ++pass) {
+      g.strips = place && pass == 1 ? 0 : strips;
+      const dim3 grid(g.strips + (place && pass == 0 ? 0 : all.x));
+      wide ? launch_wide(g, ch, grid, s) : launch_bwd<false, 0>(g, l, ch, grid, s);
+    }
+    return;
+  }
+  const bool once = streams_through((3 + (g.g_h != nullptr)) * (size_t)g.T * g.n * kActBytes);
+  const GainPlan p = gain_plan(g.T, g.n);
+  g.part = ws;
+  if (wide) {  // before g_x, which may take g_y's place
+    hipLaunchKernelGGL(k_norm_gain, dim3((g.n + 511) / 512, p.parts), dim3(256), 0, s, g, p.rows);
+    launch_wide(g, ch, all, s);
+  } else {
+    once ? launch_bwd<true, kStream>(g, l, ch, dim3(p.parts), s) : launch_bwd<true, 0>(g, l, ch, dim3(p.parts), s);
+  }
+  hipLaunchKernelGGL(k_norm_gain_sum, dim3((g.n + 31) / 32), dim3(512), 0, s, g.n, p.parts, (const float*)g.part, g.dgamma,
+                     g.accumulate);
 }
 
 // Checks and arguments shared by the two forward ops; group == 0: 16-bit (or float32) output.
@@ -858,10 +919,7 @@ int32_t resbm_skip_norm_bwd(int64_t T, int32_t n, const void* h, int64_t ld_h, c
   g.gamma = gamma, g.rstd = rstd;
   g.g_x = (act_t*)g_x, g.ld_gx = ld_gx;
   g.dgamma = dgamma, g.accumulate = accumulate;
-  if (streams_through((3 + (g_h != nullptr)) * (size_t)T * n * kActBytes))
-    run_bwd<kStream>(g, (float*)ws, (hipStream_t)stream);
-  else
-    run_bwd<0>(g, (float*)ws, (hipStream_t)stream);
+  run_bwd(g, (float*)ws, (hipStream_t)stream);
   return launch_status();
 }
 

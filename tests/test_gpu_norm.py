@@ -322,3 +322,28 @@ def test_backward_of_few_wide_rows_is_one_block_or_many(T):
             _, ref = S.norm_bwd(H, G, R_, GY)
             ref = ref + (f64(old) if acc else 0)
             within("dgamma", dg, ref, (T + 4) * U * np.sum(np.abs(GY * H * R_[:, None]), axis=0) + 2 * U * np.abs(ref) + 2.0 ** -133)
+
+
+@pytest.mark.parametrize("T", [1, 8, 128, 129, 192, 193, 256, 257, 600])
+def test_backward_around_the_rows_that_take_one_launch(T):
+    """dgamma beside the rows, or from partial sums: the bounds hold, and g_x in g_y's or g_h's place
+    gives the same bits."""
+    L = lib()
+    for n in (128, 512, 1024, 1544, 4096, 16392):
+        d = inputs(T, n, 0, L.io_dtype, 40 + T)
+        rs = torch.rsqrt((d["x"].float() ** 2).mean(1) + EPS)
+        out = []
+        for place in (None, "gy", "gh"):
+            e = {k: d[k].clone() for k in ("gy", "gh")}
+            gx = torch.empty_like(d["x"]) if place is None else e[place]
+            dg = torch.full((n,), 2.0, device="cuda")
+            L.skip_norm_bwd(d["x"], d["gamma"], rs, e["gy"], gx, dg, g_h=e["gh"], accumulate=True)
+            out.append((gx, dg))
+        for gx, dg in out[1:]:
+            assert torch.equal(gx, out[0][0]) and torch.equal(dg, out[0][1])
+        H, G, R_, GY, GH = f64(d["x"]), f64(d["gamma"]), f64(rs), f64(d["gy"]), f64(d["gh"])
+        gx, ref = S.norm_bwd(H, G, R_, GY, GH)
+        xh, w = H * R_[:, None], GY * G
+        terms = R_[:, None] * (np.abs(w) + np.abs(xh) * np.mean(np.abs(w * xh), axis=1, keepdims=True)) + np.abs(GH)
+        within("g_x", out[0][0], gx, store(L.io_dtype) * np.abs(gx) + 128 * U * terms + 2.0 ** -133)
+        within("dgamma", out[0][1], ref + 2, (T + 4) * U * np.sum(np.abs(GY * xh), axis=0) + 2 * U * np.abs(ref + 2))
