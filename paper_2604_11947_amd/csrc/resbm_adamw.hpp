@@ -71,6 +71,7 @@ struct Head {
   uint32_t magic, grads_only;
   int64_t count, chunks, bytes, traffic;  // traffic: bytes that a step reads and writes
 };
+static_assert(kThreads == 256, "block_sum adds four waves");
 static_assert(sizeof(Head) == 40 && sizeof(Entry) == 96 && sizeof(resbm_adamw_tensor) == 80, "layouts");
 
 struct Table {
@@ -367,14 +368,25 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const Entry* __restrict__ en
 
 // ---------------------------------------------------------------- gradient norm
 // Sums are float64 from the first square on: any float32 gradient's square fits.
+template <int CTRL>
+__device__ __forceinline__ double add_step(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint64_t lo = resbm_nm::dpp<CTRL>((uint32_t)u), hi = resbm_nm::dpp<CTRL>((uint32_t)(u >> 32));
+  return v + __builtin_bit_cast(double, lo | hi << 32);
+}
+__device__ __forceinline__ double of_lane(double v, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint64_t lo = (uint32_t)__builtin_amdgcn_readlane((int)u, lane);
+  const uint64_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), lane);
+  return __builtin_bit_cast(double, lo | hi << 32);
+}
 __device__ __forceinline__ double block_sum(double v, double* lds) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+  v = add_step<resbm_nm::kXor2>(add_step<resbm_nm::kXor1>(v));
+  v = add_step<resbm_nm::kMirror>(add_step<resbm_nm::kHalfMirror>(v));
+  v = (of_lane(v, 0) + of_lane(v, 16)) + (of_lane(v, 32) + of_lane(v, 48));
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
   __syncthreads();
-  double s = 0.0;
-  for (int i = 0; i < (int)(blockDim.x >> 6); ++i) s += lds[i];
-  return s;
+  return (lds[0] + lds[1]) + (lds[2] + lds[3]);  // kThreads / 64 waves
 }
 
 template <bool G16, int N>
