@@ -43,7 +43,7 @@ constexpr int kBlock = 256;            // elements per scale of an 8-bit state: 
 constexpr int kThreads = 256;
 constexpr int kTurn = kThreads * 4;    // elements that a block takes at once
 // Turns of a chunk.  float32 states: one (a block's 218 M parameters: 1106 us, with two 1167); 8-bit states, half
-// the bytes: two, with both turns' loads in flight (260 M parameters: 627 us, with one 663 and four 641);
+// the bytes: two, with both turns' loads in flight (243 M parameters: 627 us, with one 663 and four 641);
 // gradients alone: four.
 constexpr int kTurns32 = 1, kTurns8 = 2, kTurnsGrad = 4;
 constexpr int64_t kMaxBlocks = 1 << 20;
@@ -52,7 +52,7 @@ constexpr int64_t kMaxBlocks = 1 << 20;
 constexpr int kNormBlocks = 1024;
 // Shared memory that a streaming step asks for and does not touch: five blocks to a compute unit instead of
 // seven.  Five have enough loads in flight; with more the memory system serves them less evenly (218 M
-// parameters 1056 us against 1082, 260 M in 8 bits 628 against 646; four: 1066 and 658).
+// parameters 1056 us against 1082, 243 M in 8 bits 628 against 646; four: 1066 and 658).
 constexpr int kFewerBlocks = 32000;
 constexpr uint32_t kMagic = 0x57414452u;
 
