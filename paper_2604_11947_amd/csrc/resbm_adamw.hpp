@@ -14,8 +14,8 @@
 // with one float32 scale each, s = max(amax (1 / 448), 2^-126).  A block is the 256 elements that a wave takes at
 // once, so its maximum is one reduction over lanes.  u rather than v, because the square root halves the
 // exponent's range: 2^-9 .. 448 covers u over five decades, v over ten.  A non-zero u never becomes zero (it
-// rounds up to the smallest code): |m| is at most a few u, so m / u stays bounded where u is small beside
-// the block's largest, while m / (0 + eps) would not.  The step itself uses the new m and v before their rounding.
+// rounds up to the smallest code): |m| is at most a few u (for b1^2 < b2), so m / u stays bounded where u is
+// small beside the block's largest, while m / (0 + eps) would not.  The step itself uses the new m and v before their rounding.
 // Included by resbm_matrix.hip.
 #pragma once
 
