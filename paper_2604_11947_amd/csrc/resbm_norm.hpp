@@ -717,11 +717,12 @@ inline GainPlan gain_plan(int64_t T, int n) {
 // Chunks a lane.  16-bit output: one while eight waves hold the row (16384 x 4096: 90.7 us against 94.7 with
 // two chunks and 93.2 with four), four beyond (16384 x 8192: 182 against 194 with two; 5120: 116 against 118).
 // 8-bit output, with its maxima: two (16384 x 4096: 80.5 against 84 with one or four; 8192: 159 against 169
-// with four).  Few rows leave compute units idle anyway: as many lanes a row as there are chunks, to shorten
-// each one's chain.
+// with four).  Few rows leave compute units idle anyway and take a lane a chunk, to shorten each one's chain
+// (on the device, one row: 16 bits n = 8192 3.1 us against 3.3, 8 bits n = 2048 2.6 against 2.9), except 8 bits
+// above 4096, where sixteen waves meet twice (4.0 against 3.7).
 inline int chunks_fwd(int64_t T, int n, bool q8) {
   if (n > 16384) return n <= 32768 ? 4 : 8;
-  if (T <= 256 && n <= 8192) return 1;
+  if (T <= 256 && n <= (q8 ? 4096 : 8192)) return 1;
   if (q8) return 2;
   return n <= 4096 ? 1 : 4;
 }
