@@ -467,8 +467,8 @@ int32_t resbm_skip_norm_bwd(int64_t T, int32_t n, const void* h, int64_t ld_h,
  *          rather than zero.  The step uses the new m and v before that
  *          rounding.  All zeros are a valid start.  A non-finite element makes
  *          its 256 elements' states non-finite.
- * Pointers aligned to their elements; tensors whose p, g, m, v and copy are
- * 16-byte aligned take wide accesses.  numel == 0 is an entry without work.
+ * Pointers aligned to their elements (16-byte aligned ones are the fastest).
+ * numel == 0 is an entry without work.
  *
  * resbm_adamw_plan checks a list (types, NULLs, alignment, and that nothing
  * that a step writes overlaps anything else in the list) and writes the plan

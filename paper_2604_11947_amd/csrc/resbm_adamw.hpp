@@ -65,7 +65,7 @@ struct Entry {
   __bf16* copy;
   int64_t numel, first;  // first: the tensor's first chunk
   float wd;
-  int32_t g16, q8, vec, turns;  // vec: every pointer allows 16-byte (bf16: 8, codes: 4) access
+  int32_t g16, q8, turns, unused;
 };
 struct Head {
   uint32_t magic, grads_only;
@@ -94,66 +94,92 @@ __device__ __forceinline__ void from_e4m3(uint32_t q, float (&f)[4]) {
   f[0] = a.x, f[1] = a.y, f[2] = b.x, f[3] = b.y;
 }
 
+// Four elements at any address that suits one: global memory takes wide accesses without their own alignment
+// (50 M elements, float32 states: 241 us, from odd offsets 263 to 287, element by element 404; 8-bit states 146,
+// 174 and 330).
+typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u1 __attribute__((aligned(1)));
+typedef __bf16 b4 __attribute__((ext_vector_type(4), aligned(2)));
+
+// Loads and stores of global memory (pointers that come from the plan would be taken for any memory),
+// past the caches (NT) or not.
+template <class V>
+using Global = V __attribute__((address_space(1)));
+template <bool NT = false, class V>
+__device__ __forceinline__ auto get(const V* p) {
+  const Global<const V>* q = (const Global<const V>*)p;
+  if constexpr (NT) return __builtin_nontemporal_load(q);
+  return *q;
+}
+template <bool NT = false, class U, class V>
+__device__ __forceinline__ void put(U v, V* p) {
+  Global<V>* q = (Global<V>*)p;
+  if constexpr (NT)
+    __builtin_nontemporal_store(v, q);
+  else
+    *q = v;
+}
+
 // Four elements from e on, of which `left` exist; those beyond are zero.
-__device__ __forceinline__ void load_f32(const float* p, int64_t e, int left, bool vec, float (&f)[4]) {
-  if (vec && left >= 4) {
-    const float4 v = *(const float4*)(p + e);
+__device__ __forceinline__ void load_f32(const float* p, int64_t e, int left, float (&f)[4]) {
+  if (left >= 4) {
+    const f4 v = get((const f4*)(p + e));
     f[0] = v.x, f[1] = v.y, f[2] = v.z, f[3] = v.w;
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) f[i] = i < left ? p[e + i] : 0.0f;
+  for (int i = 0; i < 4; ++i) f[i] = i < left ? get(p + e + i) : 0.0f;
 }
-__device__ __forceinline__ void store_f32(float* p, int64_t e, int left, bool vec, const float (&f)[4]) {
-  if (vec && left >= 4) {
-    *(float4*)(p + e) = make_float4(f[0], f[1], f[2], f[3]);
+__device__ __forceinline__ void store_f32(float* p, int64_t e, int left, const float (&f)[4]) {
+  if (left >= 4) {
+    put(f4{f[0], f[1], f[2], f[3]}, (f4*)(p + e));
     return;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (i < left) p[e + i] = f[i];
+    if (i < left) put(f[i], p + e + i);
 }
-__device__ __forceinline__ void load_grad(const Entry& t, int64_t e, int left, bool vec, float (&f)[4]) {
-  if (!t.g16) return load_f32((const float*)t.g, e, left, vec, f);
+__device__ __forceinline__ void load_grad(const Entry& t, int64_t e, int left, float (&f)[4]) {
+  if (!t.g16) return load_f32((const float*)t.g, e, left, f);
   const uint16_t* g = (const uint16_t*)t.g;
-  if (vec && left >= 4) {
-    const uint2 v = *(const uint2*)(g + e);
+  if (left >= 4) {
+    const u2 v = get((const u2*)(g + e));
     f[0] = __builtin_bit_cast(float, v.x << 16), f[1] = __builtin_bit_cast(float, v.x & 0xFFFF0000u);
     f[2] = __builtin_bit_cast(float, v.y << 16), f[3] = __builtin_bit_cast(float, v.y & 0xFFFF0000u);
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) f[i] = i < left ? __builtin_bit_cast(float, (uint32_t)g[e + i] << 16) : 0.0f;
+  for (int i = 0; i < 4; ++i) f[i] = i < left ? __builtin_bit_cast(float, (uint32_t)get(g + e + i) << 16) : 0.0f;
 }
-__device__ __forceinline__ uint32_t load_codes(const void* p, int64_t e, int left, bool vec) {
+__device__ __forceinline__ uint32_t load_codes(const void* p, int64_t e, int left) {
   const uint8_t* q = (const uint8_t*)p + e;
-  if (vec && left >= 4) return *(const uint32_t*)q;
+  if (left >= 4) return get((const u1*)q);
   uint32_t v = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (i < left) v |= (uint32_t)q[i] << (8 * i);
+    if (i < left) v |= (uint32_t)get(q + i) << (8 * i);
   return v;
 }
-__device__ __forceinline__ void store_codes(void* p, int64_t e, int left, bool vec, uint32_t v) {
+__device__ __forceinline__ void store_codes(void* p, int64_t e, int left, uint32_t v) {
   uint8_t* q = (uint8_t*)p + e;
-  if (vec && left >= 4) {
-    *(uint32_t*)q = v;
+  if (left >= 4) {
+    put(v, (u1*)q);
     return;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (i < left) q[i] = (uint8_t)(v >> (8 * i));
+    if (i < left) put((uint8_t)(v >> (8 * i)), q + i);
 }
-__device__ __forceinline__ void store_copy(__bf16* p, int64_t e, int left, bool vec, const float (&f)[4]) {
-  typedef __bf16 c4 __attribute__((ext_vector_type(4)));
-  const c4 v = {(__bf16)f[0], (__bf16)f[1], (__bf16)f[2], (__bf16)f[3]};
-  if (vec && left >= 4) {
-    *(c4*)(p + e) = v;
+__device__ __forceinline__ void store_copy(__bf16* p, int64_t e, int left, const float (&f)[4]) {
+  const b4 v = {(__bf16)f[0], (__bf16)f[1], (__bf16)f[2], (__bf16)f[3]};
+  if (left >= 4) {
+    put(v, (b4*)(p + e));
     return;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (i < left) p[e + i] = v[i];
+    if (i < left) put(v[i], p + e + i);
 }
 
 // b^n by squaring, in float64: the bias correction of a step that only the device knows.
@@ -212,25 +238,7 @@ __device__ __forceinline__ void encode4(const float (&m)[4], const float (&u)[4]
   cu = to_e4m3(q[0], q[1], q[2], q[3]);
 }
 
-// Accesses that bypass the caches (NT), or not.
-template <bool NT, class V>
-__device__ __forceinline__ V get(const V* p) {
-  if constexpr (NT) return __builtin_nontemporal_load(p);
-  return *p;
-}
-template <bool NT, class V>
-__device__ __forceinline__ void put(V v, V* p) {
-  if constexpr (NT)
-    __builtin_nontemporal_store(v, p);
-  else
-    *p = v;
-}
-
-typedef float f4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-typedef __bf16 b4 __attribute__((ext_vector_type(4)));
-
-// A whole chunk whose pointers allow wide accesses: every load of the chunk is issued before the first use.
+// A whole chunk: every load of the chunk is issued before the first use.
 template <bool Q8, bool G16, bool NT>
 __device__ __forceinline__ void whole_chunk(const Entry& t, int64_t at, const Step& s) {
   const int lane = threadIdx.x & 63;
@@ -248,10 +256,10 @@ __device__ __forceinline__ void whole_chunk(const Entry& t, int64_t at, const St
     else
       G[k] = get<NT>((const f4*)((const float*)t.g + e));
     if constexpr (Q8) {
-      cm[k] = get<NT>((const uint32_t*)((const uint8_t*)t.m + e));
-      cu[k] = get<NT>((const uint32_t*)((const uint8_t*)t.v + e));
-      ms[k] = t.m_scale[e / kBlock];
-      us[k] = t.v_scale[e / kBlock];
+      cm[k] = get<NT>((const u1*)((const uint8_t*)t.m + e));
+      cu[k] = get<NT>((const u1*)((const uint8_t*)t.v + e));
+      ms[k] = get(t.m_scale + e / kBlock);
+      us[k] = get(t.v_scale + e / kBlock);
     } else {
       M[k] = get<NT>((const f4*)((const float*)t.m + e));
       V[k] = get<NT>((const f4*)((const float*)t.v + e));
@@ -282,11 +290,11 @@ __device__ __forceinline__ void whole_chunk(const Entry& t, int64_t at, const St
       uint32_t qm, qu;
       float sm, su;
       encode4(m, u, qm, qu, sm, su);
-      put<NT>(qm, (uint32_t*)((uint8_t*)t.m + e));
-      put<NT>(qu, (uint32_t*)((uint8_t*)t.v + e));
+      put<NT>(qm, (u1*)((uint8_t*)t.m + e));
+      put<NT>(qu, (u1*)((uint8_t*)t.v + e));
       if (lane == 0) {
-        t.m_scale[e / kBlock] = sm;
-        t.v_scale[e / kBlock] = su;
+        put(sm, t.m_scale + e / kBlock);
+        put(su, t.v_scale + e / kBlock);
       }
     } else {
       put<NT>((f4{m[0], m[1], m[2], m[3]}), (f4*)((float*)t.m + e));
@@ -295,44 +303,44 @@ __device__ __forceinline__ void whole_chunk(const Entry& t, int64_t at, const St
   }
 }
 
-// A tensor's last chunk, or one whose pointers do not: element by element where need be.
+// A tensor's last chunk, which ends inside: element by element there.
 __device__ __forceinline__ void part_chunk(const Entry& t, int64_t at, const Step& s) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const bool vec = t.vec;
   for (int k = 0; k < t.turns; ++k) {
     const int64_t w0 = at + k * kTurn + wave * kBlock;  // the wave's 256 elements
     if (w0 >= t.numel) break;
     const int64_t e = w0 + lane * 4, rest = t.numel - e;
     const int left = rest < 0 ? 0 : rest > 4 ? 4 : (int)rest;
     float p[4], g[4], m[4], v[4], u[4];
-    load_f32(t.p, e, left, vec, p);
-    load_grad(t, e, left, vec, g);
+    load_f32(t.p, e, left, p);
+    load_grad(t, e, left, g);
     if (t.q8) {
-      decode4(load_codes(t.m, e, left, vec), load_codes(t.v, e, left, vec), t.m_scale[w0 / kBlock], t.v_scale[w0 / kBlock], m, v);
+      decode4(load_codes(t.m, e, left), load_codes(t.v, e, left), get(t.m_scale + w0 / kBlock),
+              get(t.v_scale + w0 / kBlock), m, v);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (i >= left) m[i] = v[i] = 0.0f;  // beside a scale that is not finite, no element is 0 times that
     } else {
-      load_f32((const float*)t.m, e, left, vec, m);
-      load_f32((const float*)t.v, e, left, vec, v);
+      load_f32((const float*)t.m, e, left, m);
+      load_f32((const float*)t.v, e, left, v);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) step_element(s, p[i], g[i], m[i], v[i], u[i]);
-    store_f32(t.p, e, left, vec, p);
-    if (t.copy) store_copy(t.copy, e, left, vec, p);
+    store_f32(t.p, e, left, p);
+    if (t.copy) store_copy(t.copy, e, left, p);
     if (t.q8) {
       uint32_t qm, qu;
       float sm, su;
       encode4(m, u, qm, qu, sm, su);
-      store_codes(t.m, e, left, vec, qm);
-      store_codes(t.v, e, left, vec, qu);
+      store_codes(t.m, e, left, qm);
+      store_codes(t.v, e, left, qu);
       if (lane == 0) {
-        t.m_scale[w0 / kBlock] = sm;
-        t.v_scale[w0 / kBlock] = su;
+        put(sm, t.m_scale + w0 / kBlock);
+        put(su, t.v_scale + w0 / kBlock);
       }
     } else {
-      store_f32((float*)t.m, e, left, vec, m);
-      store_f32((float*)t.v, e, left, vec, v);
+      store_f32((float*)t.m, e, left, m);
+      store_f32((float*)t.v, e, left, v);
     }
   }
 }
@@ -357,7 +365,7 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const Entry* __restrict__ en
     const Entry t = entry[tensor[c]];
     const int64_t at = (c - t.first) * t.turns * kTurn;
     s.keep = (float)(1.0 - lr * (double)t.wd);
-    if (!t.vec || at + t.turns * kTurn > t.numel)
+    if (at + t.turns * kTurn > t.numel)
       part_chunk(t, at, s);
     else if (t.q8)
       t.g16 ? whole_chunk<true, true, NT>(t, at, s) : whole_chunk<true, false, NT>(t, at, s);
@@ -397,9 +405,9 @@ __device__ __forceinline__ double whole_squares(const Entry& t, int64_t at, doub
   for (int k = 0; k < N; ++k) {
     const int64_t e = at + k * kTurn + threadIdx.x * 4;
     if constexpr (G16)
-      h[k] = *(const u2*)((const uint16_t*)t.g + e);
+      h[k] = get((const u2*)((const uint16_t*)t.g + e));
     else
-      g[k] = *(const f4*)((const float*)t.g + e);
+      g[k] = get((const f4*)((const float*)t.g + e));
   }
 #pragma unroll
   for (int k = 0; k < N; ++k) {
@@ -419,7 +427,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_norm(const Entry* __restrict_
   for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
     const Entry t = entry[tensor[c]];
     const int64_t at = (c - t.first) * t.turns * kTurn;
-    if (t.vec && t.turns == kTurnsGrad && at + kTurnsGrad * kTurn <= t.numel) {
+    if (t.turns == kTurnsGrad && at + kTurnsGrad * kTurn <= t.numel) {
       s = t.g16 ? whole_squares<true, kTurnsGrad>(t, at, s) : whole_squares<false, kTurnsGrad>(t, at, s);
       continue;
     }
@@ -427,7 +435,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_norm(const Entry* __restrict_
       const int64_t e = at + k * kTurn + threadIdx.x * 4, rest = t.numel - e;
       const int left = rest < 0 ? 0 : rest > 4 ? 4 : (int)rest;
       float g[4];
-      load_grad(t, e, left, t.vec, g);
+      load_grad(t, e, left, g);
 #pragma unroll
       for (int i = 0; i < 4; ++i) s = fma((double)g[i], (double)g[i], s);
     }
@@ -584,9 +592,7 @@ int32_t resbm_adamw_plan(const resbm_adamw_tensor* tensors, int64_t count, void*
     const resbm_adamw_tensor& a = tensors[i];
     const bool q8 = a.state == RESBM_STATE_E4M3, g16 = a.g_type == RESBM_TYPE_BF16;
     e[i] = {a.p, a.g, a.m, a.v, a.m_scale, a.v_scale, (__bf16*)a.copy, a.numel, c, a.weight_decay, g16, q8,
-            aligned(a.p, 16) && aligned(a.g, g16 ? 8 : 16) && aligned(a.m, q8 ? 4 : 16) && aligned(a.v, q8 ? 4 : 16) &&
-                aligned(a.copy, 8),
-            turns_of(a)};
+            turns_of(a), 0};
     traffic += a.numel * ((g16 ? 2 : 4) + (!a.p ? 0 : 8 + (q8 ? 4 : 16) + (a.copy ? 2 : 0)));
     for (int64_t k = chunks_of(a); k > 0; --k) at[c++] = (uint32_t)i;
   }
