@@ -272,6 +272,23 @@ def test_grad_norm(sizes, g16):
             assert abs(float(out[0]) - norm) <= 1.01 * U * norm and abs(float(out[1]) - f) <= 1.01 * U * f
 
 
+def test_grad_norm_around_the_chunks_that_take_one_launch():
+    """One chunk a tensor or sixteen in one, plus and minus one, gradients of a plan with states among them."""
+    L = lib()
+    out = torch.empty(2, device="cuda")
+    for count, size in ((15, 700), (16, 4096), (17, 4096), (16, 1), (17, 3), (1, 16 * 4096), (1, 16 * 4096 + 1), (1, 4097)):
+        for g16 in (False, True):
+            d = make([size] * count, g16, seed=count)
+            for P in (L.grad_plan(d["g"]), plan(L, d, [0.0] * count)):
+                L.grad_norm(P, 2.0, out)
+                norm, f = S.grad_norm([f64(g) for g in d["g"]], 2.0)
+                assert abs(float(out[0]) - norm) <= 1.01 * U * norm and abs(float(out[1]) - f) <= 1.01 * U * f
+    d = make([512] * 5, seed=3)
+    d["g"][4][511] = float("nan")
+    L.grad_norm(L.grad_plan(d["g"]), 1.0, out)
+    assert bool(out.isnan().all())
+
+
 def test_grad_norm_of_nothing_zeros_and_large_values():
     L = lib()
     out = torch.empty(2, device="cuda")
