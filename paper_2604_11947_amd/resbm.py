@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import warnings
 
 import torch
@@ -155,6 +156,9 @@ class AdamWTensor(ctypes.Structure):
                                                                              "copy")] + [
         ("g_type", ctypes.c_int32), ("state", ctypes.c_int32), ("weight_decay", ctypes.c_float),
         ("reserved", ctypes.c_int32)]
+
+
+_ENTRY = struct.Struct("=q7Q2ifi")  # its fields in order
 
 
 class AdamWPlan:
@@ -624,27 +628,45 @@ class Library:
         if any(len(t) != k for t in lists + [decay]):
             raise ValueError("adamw_plan: lists of different lengths")
         entries = (AdamWTensor * max(k, 1))()
-        for i, (e, wd, row) in enumerate(zip(entries, decay, zip(*lists))):
+        f32, bf16, f8 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+        at, size, pack = 0, ctypes.sizeof(AdamWTensor), _ENTRY.pack_into
+        for i, (wd, row) in enumerate(zip(decay, zip(*lists))):
             P, G, M, V, ms, vs, cp = row
-            q8 = ms is not None
-            _dtype(P, torch.float32, f"p[{i}]")
-            _grad_dtype(G, i)
-            for t, nm in ((M, "m"), (V, "v")):
-                _dtype(t, torch.float8_e4m3fn if q8 else torch.float32, f"{nm}[{i}]")
-            _dtype(cp, torch.bfloat16, f"copy[{i}]")
-            if (vs is not None) != q8:
-                raise ValueError(f"m_scale[{i}], v_scale[{i}]: both or neither")
-            for t, nm in ((P, "p"), (G, "g"), (M, "m"), (V, "v"), (cp, "copy")):
-                if t is not None and (t.numel() != P.numel() or not t.is_contiguous()):
-                    raise ValueError(f"{nm}[{i}]: expected a contiguous tensor of {P.numel()} elements")
-            for t, nm in ((ms, "m_scale"), (vs, "v_scale")):
-                if t is not None:
-                    _vector(t, -(-P.numel() // STATE_BLOCK), f"{nm}[{i}]")
-            e.numel, e.weight_decay = P.numel(), wd
-            e.g_type, e.state = TYPE_BF16 if G.dtype == torch.bfloat16 else TYPE_F32, STATE_E4M3 if q8 else STATE_F32
-            for name, t in zip(("p", "g", "m", "v", "m_scale", "v_scale", "copy"), row):
-                setattr(e, name, None if t is None else t.data_ptr())
+            n, q8, g16 = P.numel(), ms is not None, G.dtype is bf16
+            state = f8 if q8 else f32
+            good = (P.dtype is f32 and (g16 or G.dtype is f32) and M.dtype is state and V.dtype is state
+                    and G.numel() == n and M.numel() == n and V.numel() == n and P.is_contiguous() and G.is_contiguous()
+                    and M.is_contiguous() and V.is_contiguous()
+                    and (cp is None or (cp.dtype is bf16 and cp.numel() == n and cp.is_contiguous())))
+            if good and q8:
+                nb = (-(-n // STATE_BLOCK),)
+                good = (vs is not None and ms.dtype is f32 and vs.dtype is f32 and ms.shape == nb and vs.shape == nb
+                        and ms.is_contiguous() and vs.is_contiguous())
+            if not good or (vs is not None) != q8:
+                self._explain_entry(i, *row)
+            pack(entries, at, n, P.data_ptr(), G.data_ptr(), M.data_ptr(), V.data_ptr(), ms.data_ptr() if q8 else 0,
+                 vs.data_ptr() if q8 else 0, 0 if cp is None else cp.data_ptr(), TYPE_BF16 if g16 else TYPE_F32,
+                 STATE_E4M3 if q8 else STATE_F32, wd, 0)
+            at += size
         return self._plan(entries, k, lists)
+
+    @staticmethod
+    def _explain_entry(i, P, G, M, V, ms, vs, cp):
+        """Raises the error of an entry that adamw_plan does not take."""
+        _dtype(P, torch.float32, f"p[{i}]")
+        _grad_dtype(G, i)
+        for t, nm in ((M, "m"), (V, "v")):
+            _dtype(t, torch.float32 if ms is None else torch.float8_e4m3fn, f"{nm}[{i}]")
+        _dtype(cp, torch.bfloat16, f"copy[{i}]")
+        if (vs is None) != (ms is None):
+            raise ValueError(f"m_scale[{i}], v_scale[{i}]: both or neither")
+        for t, nm in ((P, "p"), (G, "g"), (M, "m"), (V, "v"), (cp, "copy")):
+            if t is not None and (t.numel() != P.numel() or not t.is_contiguous()):
+                raise ValueError(f"{nm}[{i}]: expected a contiguous tensor of {P.numel()} elements")
+        for t, nm in ((ms, "m_scale"), (vs, "v_scale")):
+            if t is not None:
+                _vector(t, -(-P.numel() // STATE_BLOCK), f"{nm}[{i}]")
+        raise ValueError(f"entry {i}: not a set of tensors that a plan takes")
 
     def grad_plan(self, g) -> AdamWPlan:
         """A plan of gradients alone, for grad_norm."""
@@ -658,7 +680,7 @@ class Library:
 
     def _plan(self, entries, count, lists) -> AdamWPlan:
         tensors = [t for row in lists for t in row if t is not None]
-        if tensors:
+        if tensors and (len(set(map(torch.Tensor.get_device, tensors))) > 1 or not tensors[0].is_cuda):
             _one_gpu("plan", *tensors)
         device = tensors[0].device if tensors else torch.device("cuda", torch.cuda.current_device())
         nbytes = int(self.cdll.resbm_adamw_plan_bytes(entries, count))
