@@ -7,6 +7,7 @@ another implementation.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import struct
@@ -170,6 +171,16 @@ class AdamWPlan:
     def __init__(self, host, device_table, tensors, device):
         self.host, self.table, self.tensors, self.device = host, device_table, tensors, device
         self.host_ptr, self.table_ptr = ctypes.addressof(host), device_table.data_ptr()
+
+
+def _allocating_on(stream, device):
+    """The context in which a workspace belongs to the stream that uses it: freed with the call's return, it is
+    not handed out on another stream while the kernels run."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=device)
+    return torch.cuda.stream(stream)
 
 
 class Library:
@@ -609,7 +620,8 @@ class Library:
         ld_h, ld_gy, ld_gx = _ld(h, T, n, "h"), _ld(g_y, T, n, "g_y"), _ld(g_x, T, n, "g_x")
         ld_gh = _ld(g_h, T, n, "g_h") if g_h is not None else 0
         if ws is None:
-            ws = self.norm_workspace(T, n, h.device)
+            with _allocating_on(stream, h.device):
+                ws = self.norm_workspace(T, n, h.device)
         _one_gpu("skip_norm_bwd", h, gamma, rstd, g_y, g_x, dgamma, g_h, ws)
         st = self.cdll.resbm_skip_norm_bwd(T, n, _ptr(h), ld_h, _ptr(gamma), _ptr(rstd), _ptr(g_y), ld_gy, _ptr(g_h),
                                            ld_gh, _ptr(g_x), ld_gx, _ptr(dgamma), int(bool(accumulate)), _ptr(ws),
@@ -722,7 +734,8 @@ class Library:
         if out.device != plan.device:
             raise ValueError(f"out: expected a tensor on {plan.device}")
         if ws is None:
-            ws = self.grad_norm_workspace(plan)
+            with _allocating_on(stream, plan.device):
+                ws = self.grad_norm_workspace(plan)
         _one_gpu("grad_norm", plan.table, out, ws)
         st = self.cdll.resbm_grad_norm(plan.host_ptr, plan.table_ptr, max_norm, _ptr(out), _ptr(ws), ws.numel(),
                                        _stream(stream, plan))

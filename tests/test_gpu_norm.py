@@ -347,3 +347,30 @@ def test_backward_around_the_rows_that_take_one_launch(T):
         terms = R_[:, None] * (np.abs(w) + np.abs(xh) * np.mean(np.abs(w * xh), axis=1, keepdims=True)) + np.abs(GH)
         within("g_x", out[0][0], gx, store(L.io_dtype) * np.abs(gx) + 128 * U * terms + 2.0 ** -133)
         within("dgamma", out[0][1], ref + 2, (T + 4) * U * np.sum(np.abs(GY * xh), axis=0) + 2 * U * np.abs(ref + 2))
+
+
+def test_workspace_of_a_call_on_another_stream():
+    """Without a workspace argument, on a stream that is still busy, by object and by handle: what the caller's
+    stream allocates and writes meanwhile does not reach the sums."""
+    L = lib()
+    T, n = 2000, 2048
+    d = inputs(T, n, 0, L.io_dtype, 50)
+    rs = torch.rsqrt((d["x"].float() ** 2).mean(1) + EPS)
+    ref, gx = torch.empty(n, device="cuda"), torch.empty_like(d["x"])
+    L.skip_norm_bwd(d["x"], d["gamma"], rs, d["gy"], gx, ref)
+    P, out, norm = L.grad_plan([d["gamma"]] * 40), torch.empty(2, device="cuda"), torch.empty(2, device="cuda")
+    L.grad_norm(P, 1.0, norm)
+    torch.cuda.synchronize()
+    size = L.norm_workspace(T, n, "cuda").numel() + 256
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        dg = torch.empty(n, device="cuda")
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(2_000_000)
+        L.skip_norm_bwd(d["x"], d["gamma"], rs, d["gy"], gx, dg, stream=stream)
+        L.grad_norm(P, 1.0, out, stream=stream)
+        for _ in range(200):
+            torch.empty(size, dtype=torch.uint8, device="cuda").fill_(0xFF)
+        torch.cuda.synchronize()
+        assert torch.equal(dg, ref) and torch.equal(out, norm)
