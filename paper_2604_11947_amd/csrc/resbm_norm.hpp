@@ -456,9 +456,11 @@ struct BwdArgs {
   int strips;  // blocks that form dgamma of 64 columns each, before those that own rows
 };
 
+// With eight chunks a lane g_h is read only where it is added (1024 x 65536: 240 us; kept from the start it spilled, 275).
 template <int CH>
 struct BwdRow {
-  Act8 h[CH], gy[CH], gh[CH];
+  static constexpr int kGh = CH <= 4 ? CH : 0;
+  Act8 h[CH], gy[CH], gh[kGh ? kGh : 1];
   float rstd;
 };
 template <int POL, int L, int CH>
@@ -472,7 +474,7 @@ __device__ __forceinline__ void load_row(const BwdArgs& g, int64_t t0, const Sha
     const int c = sh.col(k);
     v.h[k] = rh.template load<POL>(c);
     v.gy[k] = ry.template load<POL>(c);
-    v.gh[k] = rg.template load<POL>(c);
+    if constexpr (BwdRow<CH>::kGh > 0) v.gh[k] = rg.template load<POL>(c);
   }
   v.rstd = g.rstd[t < g.T ? t : g.T - 1];
 }
@@ -562,12 +564,16 @@ __global__ __launch_bounds__(Shape<L>::kThreads) void k_norm_bwd(BwdArgs g) {
     }
     const float mean = team.sum(dot) / (float)g.n;
     const typename Shape<L>::template Of<act_t> ro(g.g_x, t0 + sh.sub, g.T, g.ld_gx, g.n);
+    const typename Shape<L>::template Of<const act_t> rg(g.g_h, t0 + sh.sub, g.T, g.ld_gh, g.n);
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       float f[8], v[8], u[8], a[8];
       widen(row.h[k], f);
       widen(row.gy[k], v);
-      widen(row.gh[k], u);
+      if constexpr (BwdRow<CH>::kGh > 0)
+        widen(row.gh[k], u);
+      else
+        widen(rg.template load<POL>(sh.col(k)), u);
       w.get(gain, k, lanes, lane, a);
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = (v[e] * a[e] - f[e] * row.rstd * mean) * row.rstd + u[e];
