@@ -365,23 +365,32 @@ __global__ __launch_bounds__(Shape<L>::kThreads) void k_norm_fwd(FwdArgs g) {
     const int64_t t = t0 + sh.sub;
     const In rx(g.x, t, g.T, g.ld_x, g.n), rr(g.res, t, g.T, g.ld_res, g.n), rb(g.b, t, g.T, g.r, g.r);
     const Out rh(g.h, t, g.T, g.ld_h, g.n);
-    Act8 h[CH], a[CH], b[CH];
+    // 8-bit output with eight chunks a lane reads res and b where they are added (1024 x 65536: 119 us, with all loads
+    // first it spilled, 150; 16-bit output does not: 96, and 102 the other way)
+    constexpr int AB = Q8 && CH > 4 ? 1 : CH;
+    Act8 h[CH], a[AB], b[AB];
     Gain<CH> w;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       const int c = sh.col(k);
       h[k] = rx.template load<POL>(c);
-      a[k] = rr.template load<POL>(c);
-      b[k] = rb.load_by4(c);
+      if constexpr (AB == CH) {
+        a[k] = rr.template load<POL>(c);
+        b[k] = rb.load_by4(c);
+      }
     }
     w.keep(gain, lanes, lane);
     float ss = 0.0f;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       float f[8], u[8], v[8];
+      if constexpr (AB != CH) {
+        a[0] = rr.template load<POL>(sh.col(k));
+        b[0] = rb.load_by4(sh.col(k));
+      }
       widen(h[k], f);
-      widen(a[k], u);
-      widen(b[k], v);
+      widen(a[AB == CH ? k : 0], u);
+      widen(b[AB == CH ? k : 0], v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] = f[e] + u[e] + v[e];
       h[k] = narrow(f);
