@@ -47,6 +47,7 @@ TYPE_BF16 = 1
 STATE_F32 = 0
 STATE_E4M3 = 1
 STATE_BLOCK = 256  # elements per scale of an 8-bit state
+STATE8_BETAS = (0.9, 0.95)  # the largest betas that 8-bit states follow
 
 # Newton-Schulz coefficients of the Muon method the paper cites (Sec. 3.4)
 NS_QUINTIC = (3.4445, -4.7750, 2.0315)
@@ -168,8 +169,9 @@ class AdamWPlan:
     Made by ``Library.adamw_plan`` or ``Library.grad_plan`` with the tensors' current
     addresses; a tensor that moves needs a new plan."""
 
-    def __init__(self, host, device_table, tensors, device):
+    def __init__(self, host, device_table, tensors, device, q8=False):
         self.host, self.table, self.tensors, self.device = host, device_table, tensors, device
+        self.q8 = q8  # whether there are states in 8 bits
         self.host_ptr, self.table_ptr = ctypes.addressof(host), device_table.data_ptr()
 
 
@@ -660,7 +662,7 @@ class Library:
                  vs.data_ptr() if q8 else 0, 0 if cp is None else cp.data_ptr(), TYPE_BF16 if g16 else TYPE_F32,
                  STATE_E4M3 if q8 else STATE_F32, wd, 0)
             at += size
-        return self._plan(entries, k, lists)
+        return self._plan(entries, k, lists, any(s is not None for s in lists[4]))
 
     @staticmethod
     def _explain_entry(i, P, G, M, V, ms, vs, cp):
@@ -690,7 +692,7 @@ class Library:
             e.numel, e.g, e.g_type = G.numel(), G.data_ptr(), TYPE_BF16 if G.dtype == torch.bfloat16 else TYPE_F32
         return self._plan(entries, len(g), [list(g)])
 
-    def _plan(self, entries, count, lists) -> AdamWPlan:
+    def _plan(self, entries, count, lists, q8=False) -> AdamWPlan:
         tensors = [t for row in lists for t in row if t is not None]
         if tensors and (len(set(map(torch.Tensor.get_device, tensors))) > 1 or not tensors[0].is_cuda):
             _one_gpu("plan", *tensors)
@@ -700,13 +702,16 @@ class Library:
         self._check("resbm_adamw_plan", self.cdll.resbm_adamw_plan(entries, count, host, nbytes))
         table = self._buffer(nbytes, device)
         table.copy_(torch.frombuffer(host, dtype=torch.uint8)[:nbytes])
-        return AdamWPlan(host, table, tensors, device)
+        return AdamWPlan(host, table, tensors, device, q8)
 
     def adamw_update(self, plan: AdamWPlan, lr=0.0, step=1, betas=(0.9, 0.95), eps=1e-8, grad_scale=None, lr_step=None,
                      stream=None):
         """One AdamW step on the plan's tensors.  ``grad_scale``: a float32 tensor of one element on the device, the
         gradients' factor (NaN leaves the step out); ``lr_step``: a float64 tensor {lr, step} there, read when the
-        kernel runs, in place of ``lr`` and ``step``."""
+        kernel runs, in place of ``lr`` and ``step``.  8-bit states take betas up to (0.9, 0.95): beyond, their
+        rounding would hold them where they are."""
+        if plan.q8 and (betas[0] > STATE8_BETAS[0] or betas[1] > STATE8_BETAS[1]):
+            raise ValueError(f"adamw_update: 8-bit states take betas up to {STATE8_BETAS}, got {tuple(betas)}")
         if _marshal is not None and stream is None:
             st = _marshal.adamw_update(self._at["resbm_adamw_update"], plan.host_ptr, plan.table, lr, step, betas, eps,
                                        grad_scale, lr_step)
