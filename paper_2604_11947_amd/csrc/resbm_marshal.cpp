@@ -43,10 +43,10 @@ void* packed(PyObject* o, at::ScalarType t, int64_t rows, int64_t cols) {
 void* packed_or_none(PyObject* o, at::ScalarType t, int64_t rows, int64_t cols) {
   return o == Py_None ? nullptr : packed(o, t, rows, cols);
 }
-// Rows of any stride; ld: the row stride (at least cols for a single row).
+// Contiguous rows, one or more, at any stride; ld: the row stride (at least cols for a single row).
 void* strided(PyObject* o, at::ScalarType t, int64_t rows, int64_t cols, int64_t* ld) {
   const at::Tensor& v = matrix(o, t, rows, cols);
-  need(rows <= 1 || cols <= 0 || v.stride(1) == 1);
+  need(rows <= 0 || cols <= 1 || v.stride(1) == 1);
   *ld = rows > 1 ? v.stride(0) : std::max(v.stride(0), cols);
   return v.data_ptr();
 }

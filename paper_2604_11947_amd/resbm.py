@@ -113,7 +113,7 @@ def _ptr(t):
 def _ld(t: torch.Tensor, rows: int, cols: int, name: str) -> int:
     if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
         raise ValueError(f"{name}: expected shape ({rows}, {cols}), got {tuple(t.shape)}")
-    if rows > 1 and cols > 0 and t.stride(1) != 1:
+    if rows > 0 and cols > 1 and t.stride(1) != 1:  # one row's too
         raise ValueError(f"{name}: rows must be contiguous")
     return t.stride(0) if rows > 1 else max(t.stride(0), cols)
 
