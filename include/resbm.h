@@ -480,7 +480,9 @@ int32_t resbm_skip_norm_bwd(int64_t T, int32_t n, const void* h, int64_t ld_h,
  * that a step writes overlaps anything else in the list) and writes the plan
  * to host memory, 8-byte aligned, resbm_adamw_plan_bytes bytes (0 for an
  * invalid list).  The caller copies it to device memory, 256-byte aligned, and
- * passes both; it holds addresses, so it is valid while the tensors live.
+ * passes both; it holds addresses, so it is valid while the tensors live.  Both
+ * copies have to stay until the last step has run, and the device one as long
+ * as a graph that captured a step.
  * Entries that all have only g and numel make a plan for resbm_grad_norm
  * alone.  RESBM_E_WORKSPACE: plan_bytes too small, or no host memory for the
  * check.

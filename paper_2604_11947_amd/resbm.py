@@ -167,12 +167,36 @@ class AdamWPlan:
     """A plan's host and device copies, and the tensors whose addresses it holds.
 
     Made by ``Library.adamw_plan`` or ``Library.grad_plan`` with the tensors' current
-    addresses; a tensor that moves needs a new plan."""
+    addresses; a tensor that moves needs a new plan.  A plan may be dropped while a step
+    still runs, on whichever stream (tensors that nothing else holds are the caller's to
+    keep, as for any op on another stream).  A graph that captured a step reads the plan's
+    table at every replay: the plan has to live as long as the graph."""
 
     def __init__(self, host, device_table, tensors, device, q8=False):
         self.host, self.table, self.tensors, self.device = host, device_table, tensors, device
         self.q8 = q8  # whether there are states in 8 bits
         self.host_ptr, self.table_ptr = ctypes.addressof(host), device_table.data_ptr()
+        self.streams = {_raw_stream(device)}  # that the table's memory waits for before it is used again
+
+    def used_on(self, stream):
+        """Ties the table's memory to the stream of a step: freed with the plan, it is not handed out before that
+        step has read it."""
+        raw = _raw_stream(self.device) if stream is None else int(getattr(stream, "cuda_stream", stream))
+        if raw not in self.streams:
+            self.table.record_stream(torch.cuda.current_stream(self.device) if stream is None
+                                     else _torch_stream(stream, self.device))
+            self.streams.add(raw)
+
+
+def _raw_stream(device) -> int:
+    """The handle of the device's current stream."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _torch_stream(stream, device):
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=device)
 
 
 def _allocating_on(stream, device):
@@ -180,9 +204,7 @@ def _allocating_on(stream, device):
     not handed out on another stream while the kernels run."""
     if stream is None:
         return contextlib.nullcontext()
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)), device=device)
-    return torch.cuda.stream(stream)
+    return torch.cuda.stream(_torch_stream(stream, device))
 
 
 class Library:
@@ -712,6 +734,7 @@ class Library:
         rounding would hold them where they are."""
         if plan.q8 and (betas[0] > STATE8_BETAS[0] or betas[1] > STATE8_BETAS[1]):
             raise ValueError(f"adamw_update: 8-bit states take betas up to {STATE8_BETAS}, got {tuple(betas)}")
+        plan.used_on(stream)
         if _marshal is not None and stream is None:
             st = _marshal.adamw_update(self._at["resbm_adamw_update"], plan.host_ptr, plan.table, lr, step, betas, eps,
                                        grad_scale, lr_step)
@@ -731,6 +754,7 @@ class Library:
 
     def grad_norm(self, plan: AdamWPlan, max_norm, out, ws=None, stream=None):
         """out[0] = the 2-norm of the plan's gradients, out[1] = min(1, max_norm / norm): adamw_update's grad_scale."""
+        plan.used_on(stream)
         if _marshal is not None and stream is None:
             st = _marshal.grad_norm(self._at["resbm_grad_norm"], plan.host_ptr, plan.table, max_norm, out, ws)
             if st is not None:
