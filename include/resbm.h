@@ -492,6 +492,7 @@ int32_t resbm_skip_norm_bwd(int64_t T, int32_t n, const void* h, int64_t ld_h,
  *           captured step that is replayed with other values.
  *  grad_scale  NULL, or one device float32, read when the kernel runs.  Where
  *           it is NaN the step is left out: nothing is written.
+ * Neither these nor plan_dev may overlap what the step writes.
  * 0 <= b1, b2 < 1 (and see state); 0 <= eps; step >= 1.  (With eps = 0 an element whose v is
  * zero becomes 0 / 0, NaN.)
  */
@@ -525,7 +526,7 @@ int32_t resbm_adamw_update(const void* plan, const void* plan_dev, double lr, do
  * (float64 sums in a fixed order, rounded once; max_norm > 0).  out[1] is NaN
  * where the norm is not finite, so that resbm_adamw_update with
  * grad_scale = out + 1 leaves such a step out.
- *  out  device array of two float32.
+ *  out  device array of two float32.  (Neither it nor ws may overlap a gradient.)
  *  ws   at least resbm_grad_norm_workspace_bytes(plan) bytes, 256-byte aligned.
  */
 size_t resbm_grad_norm_workspace_bytes(const void* plan);

@@ -80,9 +80,10 @@ struct Head {
   uint32_t magic;
   uint16_t grads_only, q8;  // q8: there are states in 8 bits
   int64_t count, chunks, bytes, traffic;  // traffic: bytes that a step reads and writes
+  uintptr_t lo, hi;                       // the tensors lie between
 };
 static_assert(kThreads == 256, "block_sum adds four waves");
-static_assert(sizeof(Head) == 40 && sizeof(Entry) == 96 && sizeof(resbm_adamw_tensor) == 80, "layouts");
+static_assert(sizeof(Head) == 56 && sizeof(Entry) == 96 && sizeof(resbm_adamw_tensor) == 80, "layouts");
 
 struct Table {
   const Entry* entry;
@@ -565,7 +566,8 @@ inline int32_t check_list(const resbm_adamw_tensor* t, int64_t count, int64_t* c
 
 // Nothing that a step writes may overlap anything else in the list: all ranges by address, and
 // the furthest end so far of those that are written, and of all, against the next one's start.
-inline int32_t check_overlap(const resbm_adamw_tensor* t, int64_t count) {
+// *lo and *hi: the first address and the end of all.
+inline int32_t check_overlap(const resbm_adamw_tensor* t, int64_t count, uintptr_t* lo, uintptr_t* hi) {
   Range* r = (Range*)malloc((size_t)count * 7 * sizeof(Range) + 1);
   if (!r) return RESBM_E_WORKSPACE;
   size_t k = 0;
@@ -592,6 +594,7 @@ inline int32_t check_overlap(const resbm_adamw_tensor* t, int64_t count) {
     any = r[i].end > any ? r[i].end : any;
     if (r[i].writes) written = r[i].end > written ? r[i].end : written;
   }
+  *lo = k ? r[0].at : 0, *hi = any;
   free(r);
   return clash ? RESBM_E_ALIAS : RESBM_OK;
 }
@@ -604,6 +607,24 @@ inline const Head* head_of(const void* plan) {
 inline Table table_of(const Head* h, const void* dev) {
   const char* d = (const char*)dev;
   return {(const Entry*)(d + sizeof(Head)), (const uint32_t*)(d + sizeof(Head) + h->count * sizeof(Entry))};
+}
+// Whether an operand of a call meets what the call writes (a step: p, the states, the copies) or reads (a norm:
+// the gradients) of the plan's tensors.  Most operands lie outside the span of all of them; for the others the
+// entries are looked through, about 3 ns each.
+template <bool STEP>
+inline bool meets(const Head* h, const void* p, size_t bytes) {
+  if (!p || (uintptr_t)p >= h->hi || (uintptr_t)p + bytes <= h->lo) return false;
+  const Entry* e = (const Entry*)(h + 1);
+  for (const Entry* end = e + h->count; e < end; ++e) {
+    const size_t n = (size_t)e->numel, ns = n * (e->q8 ? 1 : 4), nb = e->q8 ? (n + kBlock - 1) / kBlock * 4 : 0;
+    if (!STEP) {
+      if (overlap(p, bytes, e->g, n * (e->g16 ? 2 : 4))) return true;
+    } else if (overlap(p, bytes, e->p, n * 4) || overlap(p, bytes, e->m, ns) || overlap(p, bytes, e->v, ns) ||
+               overlap(p, bytes, e->copy, n * 2) || overlap(p, bytes, e->m_scale, nb) || overlap(p, bytes, e->v_scale, nb)) {
+      return true;
+    }
+  }
+  return false;
 }
 inline int norm_blocks(int64_t chunks) { return (int)(chunks < kNormBlocks ? chunks : kNormBlocks); }
 
@@ -628,7 +649,8 @@ int32_t resbm_adamw_plan(const resbm_adamw_tensor* tensors, int64_t count, void*
   if (!aligned(plan, 8)) return RESBM_E_ALIGN;
   const size_t bytes = plan_size(count, chunks);
   if (plan_bytes < bytes) return RESBM_E_WORKSPACE;
-  st = check_overlap(tensors, count);
+  uintptr_t lo, hi;
+  st = check_overlap(tensors, count, &lo, &hi);
   if (st != RESBM_OK) return st;
   memset(plan, 0, bytes);
   Head* h = (Head*)plan;
@@ -651,6 +673,7 @@ int32_t resbm_adamw_plan(const resbm_adamw_tensor* tensors, int64_t count, void*
   h->chunks = chunks;
   h->bytes = (int64_t)bytes;
   h->traffic = traffic;
+  h->lo = lo, h->hi = hi;
   h->magic = kMagic;
   return RESBM_OK;
 }
@@ -667,6 +690,8 @@ int32_t resbm_adamw_update(const void* plan, const void* plan_dev, double lr, do
   if (h->chunks == 0) return RESBM_OK;
   if (!plan_dev || h->grads_only) return RESBM_E_NULL;
   if (!aligned(plan_dev, 256) || !aligned(lr_step, 8) || !aligned(grad_scale, 4)) return RESBM_E_ALIGN;
+  // every block reads these, some after others have written their tensors
+  if (meets<true>(h, grad_scale, 4) || meets<true>(h, lr_step, 16) || meets<true>(h, plan_dev, h->bytes)) return RESBM_E_ALIAS;
   const double n = (double)(lr_step ? 1 : step);
   const Hyper hy = {lr, beta1, beta2, (float)beta1, (float)beta2, (float)(1.0 - beta1), (float)(1.0 - beta2), (float)eps,
                     (float)(lr / (1.0 - pow(beta1, n))), (float)(1.0 / sqrt(1.0 - pow(beta2, n))), lr_step, grad_scale};
@@ -698,7 +723,8 @@ int32_t resbm_grad_norm(const void* plan, const void* plan_dev, double max_norm,
   if (!aligned(plan_dev, 256) || !aligned(out, 4) || !aligned(ws, 256)) return RESBM_E_ALIGN;
   const size_t need = resbm_grad_norm_workspace_bytes(plan);
   if (ws_bytes < need) return RESBM_E_WORKSPACE;
-  if (overlap(out, 8, ws, need) || overlap(out, 8, plan_dev, h->bytes) || overlap(ws, need, plan_dev, h->bytes))
+  if (overlap(out, 8, ws, need) || overlap(out, 8, plan_dev, h->bytes) || overlap(ws, need, plan_dev, h->bytes) ||
+      meets<false>(h, out, 8) || meets<false>(h, ws, need))
     return RESBM_E_ALIAS;
   const Table tab = table_of(h, plan_dev);
   if (h->chunks <= kFewWaves) {
