@@ -5,10 +5,11 @@
 // for the four ops of a 256 x 512 stage with their 6 launches at 2.2 us each).
 // Each function here takes a library function's address and the op's arguments,
 // applies the binding's checks and calls it.  It returns the status, or None for
-// anything but plain CUDA tensors that pass every check (subclasses, wrapped
+// anything but plain CUDA tensors of the current device that pass every check (subclasses, wrapped
 // tensors, wrong types or shapes, no workspace): the caller then goes through
 // the Python path, which raises the error or handles the case.  Nothing is kept
 // between calls.
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <stdint.h>
@@ -85,8 +86,10 @@ int32_t dim32(int64_t v) {
 }
 void* address(PyObject* o) { return PyLong_AsVoidPtr(o); }
 
-// The current stream of t's device, as torch.cuda.current_stream gives it.
+// The current stream of t's device, as torch.cuda.current_stream gives it.  Its device has to be the current one,
+// which a launch on the default stream goes to.
 void* stream_of(const at::Tensor& t) {
+  need(c10::impl::VirtualGuardImpl(at::kCUDA).getDevice().index() == t.get_device());
   PyObject* i = PyLong_FromLong(t.get_device());
   PyObject* s = i ? PyObject_CallOneArg(g_raw_stream, i) : nullptr;
   Py_XDECREF(i);

@@ -251,6 +251,17 @@ class Library:
         if status != OK:
             raise ResbmError(op, status, self.strerror(status))
 
+    def _run(self, op: str, ref, stream, *args) -> None:
+        """Calls the library's function on `stream`, or on the current stream of the device that `ref` is on.  A launch
+        on a device's default stream goes to the current device, so that device is the current one meanwhile."""
+        s = _stream(stream, ref)
+        if ref.device.type == "cuda" and ref.device.index != torch.cuda.current_device():
+            with torch.cuda.device(ref.device):
+                st = getattr(self.cdll, op)(*args, s)
+        else:
+            st = getattr(self.cdll, op)(*args, s)
+        self._check(op, st)
+
     # ------------------------------------------------------------ ops
     def encode_fwd(self, x_attn, z, W_e, b, a_save=None, act=ACT_SILU, ws=None, stream=None):
         if _marshal is not None and stream is None:
@@ -271,9 +282,8 @@ class Library:
             _packed(a_save, T, r, "a_save")
         if ws is None:
             ws = self.workspace(T, n, r, z.device)
-        st = self.cdll.resbm_encode_fwd(T, n, r, act, _ptr(x_attn), ld_x, _ptr(z), ld_z, _ptr(W_e), _ptr(b),
-                                        _ptr(a_save), _ptr(ws), ws.numel(), _stream(stream, z))
-        self._check("resbm_encode_fwd", st)
+        self._run("resbm_encode_fwd", z, stream, T, n, r, act, _ptr(x_attn), ld_x, _ptr(z), ld_z, _ptr(W_e), _ptr(b),
+                  _ptr(a_save), _ptr(ws), ws.numel())
 
     def decode_fwd(self, b, W_d, z_tilde, add_identity=False, ws=None, stream=None):
         if _marshal is not None and stream is None:
@@ -289,9 +299,8 @@ class Library:
         _packed(W_d, r, n, "W_d")
         ld = _ld(z_tilde, T, n, "z_tilde")
         nbytes = 0 if ws is None else ws.numel()
-        st = self.cdll.resbm_decode_fwd(T, n, r, int(bool(add_identity)), _ptr(b), _ptr(W_d), _ptr(z_tilde), ld,
-                                        _ptr(ws), nbytes, _stream(stream, b))
-        self._check("resbm_decode_fwd", st)
+        self._run("resbm_decode_fwd", b, stream, T, n, r, int(bool(add_identity)), _ptr(b), _ptr(W_d), _ptr(z_tilde),
+                  ld, _ptr(ws), nbytes)
 
     def decode_bwd(self, b, W_d, g_zt, g_id, g_b, dW_d, accumulate=False, ws=None, stream=None):
         if _marshal is not None and stream is None:
@@ -314,10 +323,8 @@ class Library:
         ld_i = _ld(g_id, T, n, "g_id") if g_id is not None else 0
         if ws is None:
             ws = self.workspace(T, n, r, g_zt.device)
-        st = self.cdll.resbm_decode_bwd(T, n, r, _ptr(b), _ptr(W_d), _ptr(g_zt), ld_g, _ptr(g_id), ld_i, _ptr(g_b),
-                                        _ptr(dW_d), int(bool(accumulate)), _ptr(ws), ws.numel(),
-                                        _stream(stream, g_zt))
-        self._check("resbm_decode_bwd", st)
+        self._run("resbm_decode_bwd", g_zt, stream, T, n, r, _ptr(b), _ptr(W_d), _ptr(g_zt), ld_g, _ptr(g_id), ld_i,
+                  _ptr(g_b), _ptr(dW_d), int(bool(accumulate)), _ptr(ws), ws.numel())
 
     def encode_bwd(self, z, W_e, a_save, g_b, g_z, dW_e, g_x=None, act=ACT_SILU, accumulate=False, ws=None,
                    stream=None):
@@ -344,10 +351,8 @@ class Library:
             _packed(a_save, T, r, "a_save")
         if ws is None:
             ws = self.workspace(T, n, r, z.device)
-        st = self.cdll.resbm_encode_bwd(T, n, r, act, _ptr(z), ld_z, _ptr(W_e), _ptr(a_save), _ptr(g_b), _ptr(g_z),
-                                        ld_gz, _ptr(g_x), ld_gx, _ptr(dW_e), int(bool(accumulate)), _ptr(ws),
-                                        ws.numel(), _stream(stream, z))
-        self._check("resbm_encode_bwd", st)
+        self._run("resbm_encode_bwd", z, stream, T, n, r, act, _ptr(z), ld_z, _ptr(W_e), _ptr(a_save), _ptr(g_b),
+                  _ptr(g_z), ld_gz, _ptr(g_x), ld_gx, _ptr(dW_e), int(bool(accumulate)), _ptr(ws), ws.numel())
 
 
     def encode_bwd_noalloc(self, z, W_e, a_save, g_b, g_z, dW_e, g_x=None, act=ACT_SILU, accumulate=False,
@@ -370,10 +375,8 @@ class Library:
         _packed(dW_e, n, r, "dW_e")
         if a_save is not None:
             _packed(a_save, T, r, "a_save")
-        st = self.cdll.resbm_encode_bwd_noalloc(T, n, r, act, _ptr(z), ld_z, _ptr(W_e), _ptr(a_save), _ptr(g_b),
-                                                _ptr(g_z), ld_gz, _ptr(g_x), ld_gx, _ptr(dW_e),
-                                                int(bool(accumulate)), _stream(stream, z))
-        self._check("resbm_encode_bwd_noalloc", st)
+        self._run("resbm_encode_bwd_noalloc", z, stream, T, n, r, act, _ptr(z), ld_z, _ptr(W_e), _ptr(a_save),
+                  _ptr(g_b), _ptr(g_z), ld_gz, _ptr(g_x), ld_gx, _ptr(dW_e), int(bool(accumulate)))
 
     # ------------------------------------------------------------ two-linears-per-side ops
     # Weights W1 (n x m), W2 (m x r), W3 (r x m), W4 (m x n) and every activation
@@ -407,10 +410,8 @@ class Library:
         _packed(u, T, m, "u")
         if ws is None and act != ACT_IDENTITY:
             ws = self.two_workspace(T, n, m, r, z.device)
-        st = self.cdll.resbm2_encode_fwd(T, n, m, r, act, _ptr(x_attn), ld_x, _ptr(z), ld_z, _ptr(W1), _ptr(W2),
-                                         _ptr(b), _ptr(u), _ptr(ws), 0 if ws is None else ws.numel(),
-                                         _stream(stream, z))
-        self._check("resbm2_encode_fwd", st)
+        self._run("resbm2_encode_fwd", z, stream, T, n, m, r, act, _ptr(x_attn), ld_x, _ptr(z), ld_z, _ptr(W1),
+                  _ptr(W2), _ptr(b), _ptr(u), _ptr(ws), 0 if ws is None else ws.numel())
 
     def decode2_fwd(self, b, W3, W4, z_tilde, v, act=ACT_SILU, ws=None, stream=None):
         T = b.shape[0]
@@ -426,9 +427,8 @@ class Library:
         ld_zt = _ld(z_tilde, T, n, "z_tilde")
         if ws is None:
             ws = self.two_workspace(T, n, m, r, b.device)
-        st = self.cdll.resbm2_decode_fwd(T, n, m, r, act, _ptr(b), _ptr(W3), _ptr(W4), _ptr(z_tilde), ld_zt, _ptr(v),
-                                         _ptr(ws), ws.numel(), _stream(stream, b))
-        self._check("resbm2_decode_fwd", st)
+        self._run("resbm2_decode_fwd", b, stream, T, n, m, r, act, _ptr(b), _ptr(W3), _ptr(W4), _ptr(z_tilde), ld_zt,
+                  _ptr(v), _ptr(ws), ws.numel())
 
     def decode2_bwd(self, b, v, g_zt, g_id, W3, W4, g_b, dW3, dW4, act=ACT_SILU, ws=None, stream=None):
         T = b.shape[0]
@@ -450,10 +450,8 @@ class Library:
         ld_gid = _ld(g_id, T, n, "g_id") if g_id is not None else 0
         if ws is None:
             ws = self.two_workspace(T, n, m, r, b.device)
-        st = self.cdll.resbm2_decode_bwd(T, n, m, r, act, _ptr(b), _ptr(v), _ptr(g_zt), ld_gzt, _ptr(g_id), ld_gid,
-                                         _ptr(W3), _ptr(W4), _ptr(g_b), _ptr(dW3), _ptr(dW4), _ptr(ws), ws.numel(),
-                                         _stream(stream, b))
-        self._check("resbm2_decode_bwd", st)
+        self._run("resbm2_decode_bwd", b, stream, T, n, m, r, act, _ptr(b), _ptr(v), _ptr(g_zt), ld_gzt, _ptr(g_id),
+                  ld_gid, _ptr(W3), _ptr(W4), _ptr(g_b), _ptr(dW3), _ptr(dW4), _ptr(ws), ws.numel())
 
     def encode2_bwd(self, z, u, g_b, W1, W2, g_z, dW1, dW2, g_x=None, act=ACT_SILU, ws=None, stream=None):
         T = z.shape[0]
@@ -470,10 +468,8 @@ class Library:
         ld_gx = _ld(g_x, T, n, "g_x") if g_x is not None else 0
         if ws is None:
             ws = self.two_workspace(T, n, m, r, z.device)
-        st = self.cdll.resbm2_encode_bwd(T, n, m, r, act, _ptr(z), ld_z, _ptr(u), _ptr(g_b), _ptr(W1), _ptr(W2),
-                                         _ptr(g_z), ld_gz, _ptr(g_x), ld_gx, _ptr(dW1), _ptr(dW2), _ptr(ws),
-                                         ws.numel(), _stream(stream, z))
-        self._check("resbm2_encode_bwd", st)
+        self._run("resbm2_encode_bwd", z, stream, T, n, m, r, act, _ptr(z), ld_z, _ptr(u), _ptr(g_b), _ptr(W1),
+                  _ptr(W2), _ptr(g_z), ld_gz, _ptr(g_x), ld_gx, _ptr(dW1), _ptr(dW2), _ptr(ws), ws.numel())
 
     # ------------------------------------------------------------ encoder fused into the FFN output projection
     def ffn_encode_fwd(self, h, W_down, x_attn, W_e, z, b, a_save=None, act=ACT_SILU, ws=None, stream=None):
@@ -493,10 +489,8 @@ class Library:
             nbytes = int(self.cdll.resbm_ffn_encode_workspace_bytes(T, n, r))
             buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=h.device)
             ws = buf[(-buf.data_ptr()) % 256:][:nbytes]
-        st = self.cdll.resbm_ffn_encode_fwd(T, d_ff, n, r, act, _ptr(h), ld_h, _ptr(W_down), _ptr(x_attn), ld_x,
-                                            _ptr(W_e), _ptr(z), ld_z, _ptr(b), _ptr(a_save), _ptr(ws), ws.numel(),
-                                            _stream(stream, h))
-        self._check("resbm_ffn_encode_fwd", st)
+        self._run("resbm_ffn_encode_fwd", h, stream, T, d_ff, n, r, act, _ptr(h), ld_h, _ptr(W_down), _ptr(x_attn),
+                  ld_x, _ptr(W_e), _ptr(z), ld_z, _ptr(b), _ptr(a_save), _ptr(ws), ws.numel())
 
     def decode_qkv_fwd(self, b, W_d, gamma, W_qkv, out, eps=1e-5, ws=None, stream=None):
         T, r = b.shape
@@ -515,9 +509,8 @@ class Library:
             nbytes = int(self.cdll.resbm_decode_qkv_workspace_bytes(n, r))
             buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=b.device)
             ws = buf[(-buf.data_ptr()) % 256:][:nbytes]
-        st = self.cdll.resbm_decode_qkv_fwd(T, n, r, N, _ptr(b), _ptr(W_d), _ptr(gamma), _ptr(W_qkv), eps, _ptr(out),
-                                            ld_out, _ptr(ws), ws.numel(), _stream(stream, b))
-        self._check("resbm_decode_qkv_fwd", st)
+        self._run("resbm_decode_qkv_fwd", b, stream, T, n, r, N, _ptr(b), _ptr(W_d), _ptr(gamma), _ptr(W_qkv), eps,
+                  _ptr(out), ld_out, _ptr(ws), ws.numel())
 
     # ------------------------------------------------------------ optimizer-side ops
     def newton_schulz(self, G, O, steps=5, coeffs=NS_QUINTIC, ws=None, stream=None):
@@ -529,9 +522,7 @@ class Library:
         if ws is None:
             ws = self.matrix_workspace(p, q, G.device)
         a, b, c = coeffs
-        st = self.cdll.resbm_newton_schulz(p, q, _ptr(G), _ptr(O), steps, a, b, c, _ptr(ws), ws.numel(),
-                                           _stream(stream, G))
-        self._check("resbm_newton_schulz", st)
+        self._run("resbm_newton_schulz", G, stream, p, q, _ptr(G), _ptr(O), steps, a, b, c, _ptr(ws), ws.numel())
 
     def muon_update(self, W, G, M, lr, momentum=0.95, weight_decay=0.0, scale=None, nesterov=False, steps=5,
                     coeffs=NS_QUINTIC, ws=None, stream=None):
@@ -550,10 +541,8 @@ class Library:
         if ws is None:
             ws = self.matrix_workspace(p, q, W.device)
         a, b, c = coeffs
-        st = self.cdll.resbm_muon_update(p, q, _ptr(W), _ptr(G), _ptr(M), lr, momentum, weight_decay, scale,
-                                         int(bool(nesterov)), steps, a, b, c, _ptr(ws), ws.numel(),
-                                         _stream(stream, W))
-        self._check("resbm_muon_update", st)
+        self._run("resbm_muon_update", W, stream, p, q, _ptr(W), _ptr(G), _ptr(M), lr, momentum, weight_decay, scale,
+                  int(bool(nesterov)), steps, a, b, c, _ptr(ws), ws.numel())
 
     def spectrum(self, W, sigma, r_eff, ws=None, stream=None):
         p, q = W.shape
@@ -565,9 +554,7 @@ class Library:
             raise ValueError("sigma needs min(p, q) contiguous float64 elements, r_eff one")
         if ws is None:
             ws = self.matrix_workspace(p, q, W.device)
-        st = self.cdll.resbm_spectrum(p, q, _ptr(W), _ptr(sigma), _ptr(r_eff), _ptr(ws), ws.numel(),
-                                      _stream(stream, W))
-        self._check("resbm_spectrum", st)
+        self._run("resbm_spectrum", W, stream, p, q, _ptr(W), _ptr(sigma), _ptr(r_eff), _ptr(ws), ws.numel())
 
     # ------------------------------------------------------------ residual addition and RMS norm
     def norm_workspace(self, T: int, n: int, device) -> torch.Tensor:
@@ -603,9 +590,8 @@ class Library:
         _dtype(y, self.io_dtype, "y")
         ld_y = _ld(y, T, n, "y")
         _one_gpu("skip_norm_fwd", x, gamma, y, res, b, h, rstd)
-        st = self.cdll.resbm_skip_norm_fwd(T, n, r, _ptr(x), ld_x, _ptr(res), ld_res, _ptr(b), _ptr(gamma), eps, _ptr(h),
-                                           ld_h, _ptr(y), ld_y, _ptr(rstd), _stream(stream, x))
-        self._check("resbm_skip_norm_fwd", st)
+        self._run("resbm_skip_norm_fwd", x, stream, T, n, r, _ptr(x), ld_x, _ptr(res), ld_res, _ptr(b), _ptr(gamma),
+                  eps, _ptr(h), ld_h, _ptr(y), ld_y, _ptr(rstd))
 
     def skip_norm_q8_fwd(self, x, gamma, y, scale, res=None, b=None, h=None, rstd=None, eps=1e-5, stream=None):
         """skip_norm_fwd with y in e4m3 and float32 scales; ``scale`` (T, n / group) sets the group of columns."""
@@ -623,10 +609,8 @@ class Library:
             raise ValueError(f"scale: expected shape ({T}, n / group), got {tuple(scale.shape)}")
         _packed(scale, T, groups, "scale")
         _one_gpu("skip_norm_q8_fwd", x, gamma, y, scale, res, b, h, rstd)
-        st = self.cdll.resbm_skip_norm_q8_fwd(T, n, r, n // groups, _ptr(x), ld_x, _ptr(res), ld_res, _ptr(b),
-                                              _ptr(gamma), eps, _ptr(h), ld_h, _ptr(y), ld_y, _ptr(scale), _ptr(rstd),
-                                              _stream(stream, x))
-        self._check("resbm_skip_norm_q8_fwd", st)
+        self._run("resbm_skip_norm_q8_fwd", x, stream, T, n, r, n // groups, _ptr(x), ld_x, _ptr(res), ld_res, _ptr(b),
+                  _ptr(gamma), eps, _ptr(h), ld_h, _ptr(y), ld_y, _ptr(scale), _ptr(rstd))
 
     def skip_norm_bwd(self, h, gamma, rstd, g_y, g_x, dgamma, g_h=None, accumulate=False, ws=None, stream=None):
         """The norm's gradient plus g_h in g_x (which may be g_y or g_h), the gain's in dgamma."""
@@ -647,10 +631,8 @@ class Library:
             with _allocating_on(stream, h.device):
                 ws = self.norm_workspace(T, n, h.device)
         _one_gpu("skip_norm_bwd", h, gamma, rstd, g_y, g_x, dgamma, g_h, ws)
-        st = self.cdll.resbm_skip_norm_bwd(T, n, _ptr(h), ld_h, _ptr(gamma), _ptr(rstd), _ptr(g_y), ld_gy, _ptr(g_h),
-                                           ld_gh, _ptr(g_x), ld_gx, _ptr(dgamma), int(bool(accumulate)), _ptr(ws),
-                                           ws.numel(), _stream(stream, h))
-        self._check("resbm_skip_norm_bwd", st)
+        self._run("resbm_skip_norm_bwd", h, stream, T, n, _ptr(h), ld_h, _ptr(gamma), _ptr(rstd), _ptr(g_y), ld_gy,
+                  _ptr(g_h), ld_gh, _ptr(g_x), ld_gx, _ptr(dgamma), int(bool(accumulate)), _ptr(ws), ws.numel())
 
     # ------------------------------------------------------------ AdamW over many tensors
     def adamw_plan(self, p, g, m, v, m_scale=None, v_scale=None, copy=None, weight_decay=0.0) -> AdamWPlan:
@@ -745,9 +727,8 @@ class Library:
                 _dtype(t, dt, nm)
                 if t.numel() != k or not t.is_contiguous() or t.device != plan.device:
                     raise ValueError(f"{nm}: expected {k} contiguous elements on {plan.device}")
-        st = self.cdll.resbm_adamw_update(plan.host_ptr, plan.table_ptr, lr, betas[0], betas[1], eps, step,
-                                          _ptr(lr_step), _ptr(grad_scale), _stream(stream, plan))
-        self._check("resbm_adamw_update", st)
+        self._run("resbm_adamw_update", plan, stream, plan.host_ptr, plan.table_ptr, lr, betas[0], betas[1], eps, step,
+                  _ptr(lr_step), _ptr(grad_scale))
 
     def grad_norm_workspace(self, plan: AdamWPlan) -> torch.Tensor:
         return self._buffer(int(self.cdll.resbm_grad_norm_workspace_bytes(plan.host_ptr)), plan.device)
@@ -766,9 +747,8 @@ class Library:
             with _allocating_on(stream, plan.device):
                 ws = self.grad_norm_workspace(plan)
         _one_gpu("grad_norm", plan.table, out, ws)
-        st = self.cdll.resbm_grad_norm(plan.host_ptr, plan.table_ptr, max_norm, _ptr(out), _ptr(ws), ws.numel(),
-                                       _stream(stream, plan))
-        self._check("resbm_grad_norm", st)
+        self._run("resbm_grad_norm", plan, stream, plan.host_ptr, plan.table_ptr, max_norm, _ptr(out), _ptr(ws),
+                  ws.numel())
 
 
 _LOADED: dict[str, Library] = {}
