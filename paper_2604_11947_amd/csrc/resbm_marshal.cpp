@@ -62,7 +62,7 @@ struct Bytes {
 Bytes workspace(PyObject* o) {
   need(THPVariable_CheckExact(o));
   const at::Tensor& v = THPVariable_Unpack(o);
-  need(v.is_cuda());
+  need(v.is_cuda() && v.is_contiguous());
   return {v.data_ptr(), (size_t)v.numel()};
 }
 int32_t small_int(PyObject* o) {

@@ -110,6 +110,15 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+def _room(ws):
+    """A workspace's address and bytes."""
+    if ws is None:
+        return None, 0
+    if not ws.is_contiguous():  # an expanded one has fewer bytes than elements
+        raise ValueError(f"ws: expected a contiguous tensor, got strides {tuple(ws.stride())}")
+    return _ptr(ws), ws.numel()
+
+
 def _ld(t: torch.Tensor, rows: int, cols: int, name: str) -> int:
     if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
         raise ValueError(f"{name}: expected shape ({rows}, {cols}), got {tuple(t.shape)}")
@@ -283,7 +292,7 @@ class Library:
         if ws is None:
             ws = self.workspace(T, n, r, z.device)
         self._run("resbm_encode_fwd", z, stream, T, n, r, act, _ptr(x_attn), ld_x, _ptr(z), ld_z, _ptr(W_e), _ptr(b),
-                  _ptr(a_save), _ptr(ws), ws.numel())
+                  _ptr(a_save), *_room(ws))
 
     def decode_fwd(self, b, W_d, z_tilde, add_identity=False, ws=None, stream=None):
         if _marshal is not None and stream is None:
@@ -298,9 +307,8 @@ class Library:
         _packed(b, T, r, "b")
         _packed(W_d, r, n, "W_d")
         ld = _ld(z_tilde, T, n, "z_tilde")
-        nbytes = 0 if ws is None else ws.numel()
         self._run("resbm_decode_fwd", b, stream, T, n, r, int(bool(add_identity)), _ptr(b), _ptr(W_d), _ptr(z_tilde),
-                  ld, _ptr(ws), nbytes)
+                  ld, *_room(ws))
 
     def decode_bwd(self, b, W_d, g_zt, g_id, g_b, dW_d, accumulate=False, ws=None, stream=None):
         if _marshal is not None and stream is None:
@@ -324,7 +332,7 @@ class Library:
         if ws is None:
             ws = self.workspace(T, n, r, g_zt.device)
         self._run("resbm_decode_bwd", g_zt, stream, T, n, r, _ptr(b), _ptr(W_d), _ptr(g_zt), ld_g, _ptr(g_id), ld_i,
-                  _ptr(g_b), _ptr(dW_d), int(bool(accumulate)), _ptr(ws), ws.numel())
+                  _ptr(g_b), _ptr(dW_d), int(bool(accumulate)), *_room(ws))
 
     def encode_bwd(self, z, W_e, a_save, g_b, g_z, dW_e, g_x=None, act=ACT_SILU, accumulate=False, ws=None,
                    stream=None):
@@ -352,7 +360,7 @@ class Library:
         if ws is None:
             ws = self.workspace(T, n, r, z.device)
         self._run("resbm_encode_bwd", z, stream, T, n, r, act, _ptr(z), ld_z, _ptr(W_e), _ptr(a_save), _ptr(g_b),
-                  _ptr(g_z), ld_gz, _ptr(g_x), ld_gx, _ptr(dW_e), int(bool(accumulate)), _ptr(ws), ws.numel())
+                  _ptr(g_z), ld_gz, _ptr(g_x), ld_gx, _ptr(dW_e), int(bool(accumulate)), *_room(ws))
 
 
     def encode_bwd_noalloc(self, z, W_e, a_save, g_b, g_z, dW_e, g_x=None, act=ACT_SILU, accumulate=False,
@@ -411,7 +419,7 @@ class Library:
         if ws is None and act != ACT_IDENTITY:
             ws = self.two_workspace(T, n, m, r, z.device)
         self._run("resbm2_encode_fwd", z, stream, T, n, m, r, act, _ptr(x_attn), ld_x, _ptr(z), ld_z, _ptr(W1),
-                  _ptr(W2), _ptr(b), _ptr(u), _ptr(ws), 0 if ws is None else ws.numel())
+                  _ptr(W2), _ptr(b), _ptr(u), *_room(ws))
 
     def decode2_fwd(self, b, W3, W4, z_tilde, v, act=ACT_SILU, ws=None, stream=None):
         T = b.shape[0]
@@ -428,7 +436,7 @@ class Library:
         if ws is None:
             ws = self.two_workspace(T, n, m, r, b.device)
         self._run("resbm2_decode_fwd", b, stream, T, n, m, r, act, _ptr(b), _ptr(W3), _ptr(W4), _ptr(z_tilde), ld_zt,
-                  _ptr(v), _ptr(ws), ws.numel())
+                  _ptr(v), *_room(ws))
 
     def decode2_bwd(self, b, v, g_zt, g_id, W3, W4, g_b, dW3, dW4, act=ACT_SILU, ws=None, stream=None):
         T = b.shape[0]
@@ -451,7 +459,7 @@ class Library:
         if ws is None:
             ws = self.two_workspace(T, n, m, r, b.device)
         self._run("resbm2_decode_bwd", b, stream, T, n, m, r, act, _ptr(b), _ptr(v), _ptr(g_zt), ld_gzt, _ptr(g_id),
-                  ld_gid, _ptr(W3), _ptr(W4), _ptr(g_b), _ptr(dW3), _ptr(dW4), _ptr(ws), ws.numel())
+                  ld_gid, _ptr(W3), _ptr(W4), _ptr(g_b), _ptr(dW3), _ptr(dW4), *_room(ws))
 
     def encode2_bwd(self, z, u, g_b, W1, W2, g_z, dW1, dW2, g_x=None, act=ACT_SILU, ws=None, stream=None):
         T = z.shape[0]
@@ -469,7 +477,7 @@ class Library:
         if ws is None:
             ws = self.two_workspace(T, n, m, r, z.device)
         self._run("resbm2_encode_bwd", z, stream, T, n, m, r, act, _ptr(z), ld_z, _ptr(u), _ptr(g_b), _ptr(W1),
-                  _ptr(W2), _ptr(g_z), ld_gz, _ptr(g_x), ld_gx, _ptr(dW1), _ptr(dW2), _ptr(ws), ws.numel())
+                  _ptr(W2), _ptr(g_z), ld_gz, _ptr(g_x), ld_gx, _ptr(dW1), _ptr(dW2), *_room(ws))
 
     # ------------------------------------------------------------ encoder fused into the FFN output projection
     def ffn_encode_fwd(self, h, W_down, x_attn, W_e, z, b, a_save=None, act=ACT_SILU, ws=None, stream=None):
@@ -490,7 +498,7 @@ class Library:
             buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=h.device)
             ws = buf[(-buf.data_ptr()) % 256:][:nbytes]
         self._run("resbm_ffn_encode_fwd", h, stream, T, d_ff, n, r, act, _ptr(h), ld_h, _ptr(W_down), _ptr(x_attn),
-                  ld_x, _ptr(W_e), _ptr(z), ld_z, _ptr(b), _ptr(a_save), _ptr(ws), ws.numel())
+                  ld_x, _ptr(W_e), _ptr(z), ld_z, _ptr(b), _ptr(a_save), *_room(ws))
 
     def decode_qkv_fwd(self, b, W_d, gamma, W_qkv, out, eps=1e-5, ws=None, stream=None):
         T, r = b.shape
@@ -510,7 +518,7 @@ class Library:
             buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=b.device)
             ws = buf[(-buf.data_ptr()) % 256:][:nbytes]
         self._run("resbm_decode_qkv_fwd", b, stream, T, n, r, N, _ptr(b), _ptr(W_d), _ptr(gamma), _ptr(W_qkv), eps,
-                  _ptr(out), ld_out, _ptr(ws), ws.numel())
+                  _ptr(out), ld_out, *_room(ws))
 
     # ------------------------------------------------------------ optimizer-side ops
     def newton_schulz(self, G, O, steps=5, coeffs=NS_QUINTIC, ws=None, stream=None):
@@ -522,7 +530,7 @@ class Library:
         if ws is None:
             ws = self.matrix_workspace(p, q, G.device)
         a, b, c = coeffs
-        self._run("resbm_newton_schulz", G, stream, p, q, _ptr(G), _ptr(O), steps, a, b, c, _ptr(ws), ws.numel())
+        self._run("resbm_newton_schulz", G, stream, p, q, _ptr(G), _ptr(O), steps, a, b, c, *_room(ws))
 
     def muon_update(self, W, G, M, lr, momentum=0.95, weight_decay=0.0, scale=None, nesterov=False, steps=5,
                     coeffs=NS_QUINTIC, ws=None, stream=None):
@@ -542,7 +550,7 @@ class Library:
             ws = self.matrix_workspace(p, q, W.device)
         a, b, c = coeffs
         self._run("resbm_muon_update", W, stream, p, q, _ptr(W), _ptr(G), _ptr(M), lr, momentum, weight_decay, scale,
-                  int(bool(nesterov)), steps, a, b, c, _ptr(ws), ws.numel())
+                  int(bool(nesterov)), steps, a, b, c, *_room(ws))
 
     def spectrum(self, W, sigma, r_eff, ws=None, stream=None):
         p, q = W.shape
@@ -554,7 +562,7 @@ class Library:
             raise ValueError("sigma needs min(p, q) contiguous float64 elements, r_eff one")
         if ws is None:
             ws = self.matrix_workspace(p, q, W.device)
-        self._run("resbm_spectrum", W, stream, p, q, _ptr(W), _ptr(sigma), _ptr(r_eff), _ptr(ws), ws.numel())
+        self._run("resbm_spectrum", W, stream, p, q, _ptr(W), _ptr(sigma), _ptr(r_eff), *_room(ws))
 
     # ------------------------------------------------------------ residual addition and RMS norm
     def norm_workspace(self, T: int, n: int, device) -> torch.Tensor:
@@ -632,7 +640,7 @@ class Library:
                 ws = self.norm_workspace(T, n, h.device)
         _one_gpu("skip_norm_bwd", h, gamma, rstd, g_y, g_x, dgamma, g_h, ws)
         self._run("resbm_skip_norm_bwd", h, stream, T, n, _ptr(h), ld_h, _ptr(gamma), _ptr(rstd), _ptr(g_y), ld_gy,
-                  _ptr(g_h), ld_gh, _ptr(g_x), ld_gx, _ptr(dgamma), int(bool(accumulate)), _ptr(ws), ws.numel())
+                  _ptr(g_h), ld_gh, _ptr(g_x), ld_gx, _ptr(dgamma), int(bool(accumulate)), *_room(ws))
 
     # ------------------------------------------------------------ AdamW over many tensors
     def adamw_plan(self, p, g, m, v, m_scale=None, v_scale=None, copy=None, weight_decay=0.0) -> AdamWPlan:
@@ -747,8 +755,7 @@ class Library:
             with _allocating_on(stream, plan.device):
                 ws = self.grad_norm_workspace(plan)
         _one_gpu("grad_norm", plan.table, out, ws)
-        self._run("resbm_grad_norm", plan, stream, plan.host_ptr, plan.table_ptr, max_norm, _ptr(out), _ptr(ws),
-                  ws.numel())
+        self._run("resbm_grad_norm", plan, stream, plan.host_ptr, plan.table_ptr, max_norm, _ptr(out), *_room(ws))
 
 
 _LOADED: dict[str, Library] = {}
