@@ -387,7 +387,8 @@ int32_t resbm_decode_qkv_fwd(int64_t T, int32_t n, int32_t r, int32_t N,
  *     y[t][c] = h[t][c] rstd[t] gamma[c],  rstd[t] = 1 / sqrt(mean_c h[t][c]^2 + eps)
  * The sum is formed in float32 in that order and rounded once to act; the norm
  * is that of the rounded h, whether h is written or not, in float32 (a row
- * whose mean square exceeds float32's range gets rstd = 0); y is rounded once.
+ * whose mean square exceeds float32's range gets rstd = 0; with eps = 0 one
+ * whose mean square is zero there gets an infinite rstd); y is rounded once.
  *  x      T x n act, row stride ld_x.
  *  res    T x n act, row stride ld_res, or NULL.
  *  b      T x r act, packed [T][r]; r == 0: none (b may be NULL).
@@ -435,7 +436,8 @@ int32_t resbm_skip_norm_q8_fwd(int64_t T, int32_t n, int32_t r, int32_t group,
  *         norm, or NULL.
  *  g_x    out, T x n act, row stride ld_gx; may take the place of g_y or g_h.
  *  dgamma n float32, overwritten or accumulated into; fixed order of the token
- *         sum.  (T == 0 leaves it as it is, as in every op.)
+ *         sum.  (T == 0 leaves it as it is, as in every op: a caller whose batch
+ *         may be empty clears it first and accumulates.)
  *  ws     at least resbm_norm_workspace_bytes(T, n) bytes.
  */
 size_t resbm_norm_workspace_bytes(int64_t T, int32_t n);
@@ -524,8 +526,14 @@ int32_t resbm_adamw_update(const void* plan, const void* plan_dev, double lr, do
  * The 2-norm of all gradients of a plan and the factor that clips it:
  *     out[0] = sqrt(sum g^2),   out[1] = min(1, max_norm / (norm + 1e-6))
  * (float64 sums in a fixed order, rounded once; max_norm > 0).  out[1] is NaN
- * where the norm is not finite, so that resbm_adamw_update with
+ * where the norm is not finite in float64, so that resbm_adamw_update with
  * grad_scale = out + 1 leaves such a step out.
+ * A plan of the gradients alone is the faster one to take (218 M gradients:
+ * 136 us against 217 over a plan with float32 states).
+ * This is the norm of one plan.  To clip by the norm over several plans or
+ * pipeline stages, add the squares of their out[0] (all-reduce them between
+ * ranks), form the factor from the root as above, NaN where that is not
+ * finite, and pass it as each step's grad_scale.
  *  out  device array of two float32.  (Neither it nor ws may overlap a gradient.)
  *  ws   at least resbm_grad_norm_workspace_bytes(plan) bytes, 256-byte aligned.
  */

@@ -172,6 +172,9 @@ class AdamWTensor(ctypes.Structure):
 _ENTRY = struct.Struct("=q7Q2ifi")  # its fields in order
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # a device's current stream, as a handle
+
+
 class AdamWPlan:
     """A plan's host and device copies, and the tensors whose addresses it holds.
 
@@ -185,21 +188,17 @@ class AdamWPlan:
         self.host, self.table, self.tensors, self.device = host, device_table, tensors, device
         self.q8 = q8  # whether there are states in 8 bits
         self.host_ptr, self.table_ptr = ctypes.addressof(host), device_table.data_ptr()
-        self.streams = {_raw_stream(device)}  # that the table's memory waits for before it is used again
+        self.index = device.index
+        self.streams = {_raw_stream(self.index)}  # that the table's memory waits for before it is used again
 
     def used_on(self, stream):
         """Ties the table's memory to the stream of a step: freed with the plan, it is not handed out before that
         step has read it."""
-        raw = _raw_stream(self.device) if stream is None else int(getattr(stream, "cuda_stream", stream))
+        raw = _raw_stream(self.index) if stream is None else int(getattr(stream, "cuda_stream", stream))
         if raw not in self.streams:
             self.table.record_stream(torch.cuda.current_stream(self.device) if stream is None
                                      else _torch_stream(stream, self.device))
             self.streams.add(raw)
-
-
-def _raw_stream(device) -> int:
-    """The handle of the device's current stream."""
-    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _torch_stream(stream, device):
@@ -646,7 +645,9 @@ class Library:
     def adamw_plan(self, p, g, m, v, m_scale=None, v_scale=None, copy=None, weight_decay=0.0) -> AdamWPlan:
         """The plan of the lists' tensors: float32 ``p``, gradients float32 or bf16, states float32 or, with
         ``m_scale`` and ``v_scale`` (an entry may be None), float8_e4m3fn; ``copy``: bf16 tensors or None.
-        It copies its table to the device, so it is made outside a graph capture; its updates may be captured."""
+        It copies its table to the device, so it is made outside a graph capture; its updates may be captured.
+        It holds addresses: gradients stay where they are (``zero_grad(set_to_none=False)``), or a new plan is made
+        for the new ones; until it goes, it keeps its tensors."""
         k = len(p)
         none = [None] * k
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * k
@@ -742,7 +743,8 @@ class Library:
         return self._buffer(int(self.cdll.resbm_grad_norm_workspace_bytes(plan.host_ptr)), plan.device)
 
     def grad_norm(self, plan: AdamWPlan, max_norm, out, ws=None, stream=None):
-        """out[0] = the 2-norm of the plan's gradients, out[1] = min(1, max_norm / norm): adamw_update's grad_scale."""
+        """out[0] = the 2-norm of the plan's gradients, out[1] = min(1, max_norm / norm): adamw_update's grad_scale.
+        Over several plans or ranks: the root of the sum of their squared out[0], and the factor from that."""
         plan.used_on(stream)
         if _marshal is not None and stream is None:
             st = _marshal.grad_norm(self._at["resbm_grad_norm"], plan.host_ptr, plan.table, max_norm, out, ws)
