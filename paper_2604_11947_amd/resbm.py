@@ -289,7 +289,8 @@ class Library:
         if a_save is not None:
             _packed(a_save, T, r, "a_save")
         if ws is None:
-            ws = self.workspace(T, n, r, z.device)
+            with _allocating_on(stream, z.device):
+                ws = self.workspace(T, n, r, z.device)
         self._run("resbm_encode_fwd", z, stream, T, n, r, act, _ptr(x_attn), ld_x, _ptr(z), ld_z, _ptr(W_e), _ptr(b),
                   _ptr(a_save), *_room(ws))
 
@@ -329,7 +330,8 @@ class Library:
         ld_g = _ld(g_zt, T, n, "g_zt")
         ld_i = _ld(g_id, T, n, "g_id") if g_id is not None else 0
         if ws is None:
-            ws = self.workspace(T, n, r, g_zt.device)
+            with _allocating_on(stream, g_zt.device):
+                ws = self.workspace(T, n, r, g_zt.device)
         self._run("resbm_decode_bwd", g_zt, stream, T, n, r, _ptr(b), _ptr(W_d), _ptr(g_zt), ld_g, _ptr(g_id), ld_i,
                   _ptr(g_b), _ptr(dW_d), int(bool(accumulate)), *_room(ws))
 
@@ -357,7 +359,8 @@ class Library:
         if a_save is not None:
             _packed(a_save, T, r, "a_save")
         if ws is None:
-            ws = self.workspace(T, n, r, z.device)
+            with _allocating_on(stream, z.device):
+                ws = self.workspace(T, n, r, z.device)
         self._run("resbm_encode_bwd", z, stream, T, n, r, act, _ptr(z), ld_z, _ptr(W_e), _ptr(a_save), _ptr(g_b),
                   _ptr(g_z), ld_gz, _ptr(g_x), ld_gx, _ptr(dW_e), int(bool(accumulate)), *_room(ws))
 
@@ -416,7 +419,8 @@ class Library:
         _packed(b, T, r, "b")
         _packed(u, T, m, "u")
         if ws is None and act != ACT_IDENTITY:
-            ws = self.two_workspace(T, n, m, r, z.device)
+            with _allocating_on(stream, z.device):
+                ws = self.two_workspace(T, n, m, r, z.device)
         self._run("resbm2_encode_fwd", z, stream, T, n, m, r, act, _ptr(x_attn), ld_x, _ptr(z), ld_z, _ptr(W1),
                   _ptr(W2), _ptr(b), _ptr(u), *_room(ws))
 
@@ -433,7 +437,8 @@ class Library:
         _packed(v, T, m, "v")
         ld_zt = _ld(z_tilde, T, n, "z_tilde")
         if ws is None:
-            ws = self.two_workspace(T, n, m, r, b.device)
+            with _allocating_on(stream, b.device):
+                ws = self.two_workspace(T, n, m, r, b.device)
         self._run("resbm2_decode_fwd", b, stream, T, n, m, r, act, _ptr(b), _ptr(W3), _ptr(W4), _ptr(z_tilde), ld_zt,
                   _ptr(v), *_room(ws))
 
@@ -456,7 +461,8 @@ class Library:
         ld_gzt = _ld(g_zt, T, n, "g_zt")
         ld_gid = _ld(g_id, T, n, "g_id") if g_id is not None else 0
         if ws is None:
-            ws = self.two_workspace(T, n, m, r, b.device)
+            with _allocating_on(stream, b.device):
+                ws = self.two_workspace(T, n, m, r, b.device)
         self._run("resbm2_decode_bwd", b, stream, T, n, m, r, act, _ptr(b), _ptr(v), _ptr(g_zt), ld_gzt, _ptr(g_id),
                   ld_gid, _ptr(W3), _ptr(W4), _ptr(g_b), _ptr(dW3), _ptr(dW4), *_room(ws))
 
@@ -474,7 +480,8 @@ class Library:
         ld_z, ld_gz = _ld(z, T, n, "z"), _ld(g_z, T, n, "g_z")
         ld_gx = _ld(g_x, T, n, "g_x") if g_x is not None else 0
         if ws is None:
-            ws = self.two_workspace(T, n, m, r, z.device)
+            with _allocating_on(stream, z.device):
+                ws = self.two_workspace(T, n, m, r, z.device)
         self._run("resbm2_encode_bwd", z, stream, T, n, m, r, act, _ptr(z), ld_z, _ptr(u), _ptr(g_b), _ptr(W1),
                   _ptr(W2), _ptr(g_z), ld_gz, _ptr(g_x), ld_gx, _ptr(dW1), _ptr(dW2), *_room(ws))
 
@@ -494,8 +501,8 @@ class Library:
         ld_h, ld_x, ld_z = _ld(h, T, d_ff, "h"), _ld(x_attn, T, n, "x_attn"), _ld(z, T, n, "z")
         if ws is None:
             nbytes = int(self.cdll.resbm_ffn_encode_workspace_bytes(T, n, r))
-            buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=h.device)
-            ws = buf[(-buf.data_ptr()) % 256:][:nbytes]
+            with _allocating_on(stream, h.device):
+                ws = self._buffer(nbytes, h.device)
         self._run("resbm_ffn_encode_fwd", h, stream, T, d_ff, n, r, act, _ptr(h), ld_h, _ptr(W_down), _ptr(x_attn),
                   ld_x, _ptr(W_e), _ptr(z), ld_z, _ptr(b), _ptr(a_save), *_room(ws))
 
@@ -514,8 +521,8 @@ class Library:
         ld_out = _ld(out, T, N, "out")
         if ws is None:
             nbytes = int(self.cdll.resbm_decode_qkv_workspace_bytes(n, r))
-            buf = torch.empty(nbytes + 256, dtype=torch.uint8, device=b.device)
-            ws = buf[(-buf.data_ptr()) % 256:][:nbytes]
+            with _allocating_on(stream, b.device):
+                ws = self._buffer(nbytes, b.device)
         self._run("resbm_decode_qkv_fwd", b, stream, T, n, r, N, _ptr(b), _ptr(W_d), _ptr(gamma), _ptr(W_qkv), eps,
                   _ptr(out), ld_out, *_room(ws))
 
@@ -527,7 +534,8 @@ class Library:
         _packed(G, p, q, "G")
         _packed(O, p, q, "O")
         if ws is None:
-            ws = self.matrix_workspace(p, q, G.device)
+            with _allocating_on(stream, G.device):
+                ws = self.matrix_workspace(p, q, G.device)
         a, b, c = coeffs
         self._run("resbm_newton_schulz", G, stream, p, q, _ptr(G), _ptr(O), steps, a, b, c, *_room(ws))
 
@@ -546,7 +554,8 @@ class Library:
         if scale is None:
             scale = -1.0  # the library's default (negative selects it)
         if ws is None:
-            ws = self.matrix_workspace(p, q, W.device)
+            with _allocating_on(stream, W.device):
+                ws = self.matrix_workspace(p, q, W.device)
         a, b, c = coeffs
         self._run("resbm_muon_update", W, stream, p, q, _ptr(W), _ptr(G), _ptr(M), lr, momentum, weight_decay, scale,
                   int(bool(nesterov)), steps, a, b, c, *_room(ws))
@@ -560,7 +569,8 @@ class Library:
         if sigma.numel() < min(p, q) or r_eff.numel() < 1 or not sigma.is_contiguous():
             raise ValueError("sigma needs min(p, q) contiguous float64 elements, r_eff one")
         if ws is None:
-            ws = self.matrix_workspace(p, q, W.device)
+            with _allocating_on(stream, W.device):
+                ws = self.matrix_workspace(p, q, W.device)
         self._run("resbm_spectrum", W, stream, p, q, _ptr(W), _ptr(sigma), _ptr(r_eff), *_room(ws))
 
     # ------------------------------------------------------------ residual addition and RMS norm
@@ -675,7 +685,7 @@ class Library:
                  vs.data_ptr() if q8 else 0, 0 if cp is None else cp.data_ptr(), TYPE_BF16 if g16 else TYPE_F32,
                  STATE_E4M3 if q8 else STATE_F32, wd, 0)
             at += size
-        return self._plan(entries, k, lists, any(s is not None for s in lists[4]))
+        return self._plan(entries, k, lists, any(s is not None and s.numel() > 0 for s in lists[4]))
 
     @staticmethod
     def _explain_entry(i, P, G, M, V, ms, vs, cp):
