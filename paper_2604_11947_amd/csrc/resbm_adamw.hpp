@@ -610,7 +610,7 @@ inline Table table_of(const Head* h, const void* dev) {
 }
 // Whether an operand of a call meets what the call writes (a step: p, the states, the copies) or reads (a norm:
 // the gradients) of the plan's tensors.  Most operands lie outside the span of all of them; for the others the
-// entries are looked through, about 3 ns each.
+// entries are looked through (a norm's two operands among 400 tensors: 0.9 us of host time).
 template <bool STEP>
 inline bool meets(const Head* h, const void* p, size_t bytes) {
   if (!p || (uintptr_t)p >= h->hi || (uintptr_t)p + bytes <= h->lo) return false;
